@@ -169,6 +169,78 @@ int amla_mla_decode_fp8(const void* q, const void* kv_cache_e4m3, float kv_scale
                         int max_blocks_per_seq, void* out, float* lse, void* workspace, size_t workspace_bytes,
                         void* cuda_stream, int flags);
 
+/*
+ * The same decode on a cache held in 4 bits (no counterpart in the paper).
+ *
+ *   kv_cache_fp4   device, uint8 [num_blocks, 20736], 16-byte aligned.  A page is 64 keys: 64 rows of 288 bytes of E2M1 numbers
+ *                  (sign, 2 exponent bits with bias 1, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), two to a byte with the lower
+ *                  column in the low half, then 64 rows of 36 E4M3 scales, one for each 16 columns.  The value of an
+ *                  element is e2m1 * e4m3 * kv_scale; its first 512 columns are V.  amla_cache_store_fp4 writes such rows.
+ *   kv_scale       one factor for the whole cache, 2^-100 .. 2^100
+ *   workspace      at least amla_mla_decode_fp4_workspace_size() bytes, 256-byte aligned
+ *
+ * A call reads 324 bytes a key (bf16: 1152).  Rows of a used page beyond the sequence length may hold anything.  A block-table entry outside [0, num_blocks) of a used page reads
+ * as a page of zeros.  Everything else (visibility rule, outputs, shapes, errors) is as for amla_mla_decode; amla_check_status reads the status.
+ */
+int amla_mla_decode_fp4_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int device, size_t* bytes_out);
+int amla_mla_decode_fp4(const void* q, const void* kv_cache_fp4, float kv_scale, const int32_t* block_table,
+                        const int32_t* seqlens, float softmax_scale, int B, int Sq, int H, int num_blocks,
+                        int max_blocks_per_seq, void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Tokens into a 4-bit cache, and back.  The batch's tokens are rows of 576 bf16, `row_stride` elements apart (>= 576; rows that
+ * begin at 16 bytes are accessed whole): tokens starts[b] .. starts[b+1] - 1 are the LAST starts[b+1] - starts[b] of the
+ * seqlens[b] of sequence b, in order, so that a decode step, a prompt's chunk and a ragged batch of both are one call.
+ * `starts` is a device array of B + 1 that does not fall; tokens outside [starts[0], starts[B]), in front of a sequence's first
+ * position, beyond the table or in a page outside [0, num_blocks) are not stored, and read back as zeros.
+ *
+ * store: for each 16 columns, scale = e4m3(max |x| / (6 kv_scale)) and e2m1(x / (scale kv_scale)), both to nearest with ties to
+ * even, both saturating.  A group that holds a NaN reads back as NaN.  Two tokens of a call must not have the same place.
+ * load:  out = bf16(e2m1 * e4m3 * kv_scale), what the decode call sees.
+ */
+int amla_cache_store_fp4(const void* kv, long long row_stride, int n_tokens, const int32_t* starts, void* kv_cache_fp4,
+                         float kv_scale, const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks,
+                         int max_blocks_per_seq, void* cuda_stream);
+int amla_cache_load_fp4(const void* kv_cache_fp4, float kv_scale, const int32_t* block_table, const int32_t* seqlens,
+                        const int32_t* starts, int B, int num_blocks, int max_blocks_per_seq, void* out, long long row_stride,
+                        int n_tokens, void* cuda_stream);
+
+/*
+ * Care of a cache's pages, on the device: no length, count or page number is read on the host, so that all of it can be enqueued
+ * (or replayed from a graph) between decode calls.  A cache is num_blocks pages of page_bytes (a multiple of 16: bf16 73 728, E4M3
+ * 36 864, 4 bits 20 736), 16-byte aligned.  Its books are
+ *   block_table  int32 [B, max_blocks_per_seq], row b: the pages of sequence b in its first ceil(seqlens[b] / 64) entries
+ *   seqlens      int32 [B]
+ *   refs         int32 [num_blocks]: in how many entries a page is named; a page is free if it is in none (refs <= 0)
+ * Pages are handed out lowest first, in the order of the requests; calls that change the books are ordered by their stream.
+ * `workspace`: 256-byte aligned, at least amla_pages_workspace_size() bytes, contents need not be kept or initialised.
+ *
+ * copy     page dst[i] becomes page src[i] (n pairs; one with an index outside the cache is skipped).  No dst may be a src of another
+ *          pair, or a dst twice.
+ * free     the listed rows give up their pages and are left empty (entries -1, length 0).  A row that is listed twice is freed once;
+ *          an index outside [0, B) is skipped.
+ * fork     row children[i] becomes a copy of row parents[i]: it shares the full pages (refs + 1) and has a copy of a last page that is
+ *          not full, in a free page, so that either may go on writing.  A child's row is overwritten: it should be empty (freed).
+ *          No child may be a parent, or a child twice.  served[i] (or NULL): 1, or 0 where a page was needed and none was
+ *          left (the child is then empty) or an index is outside [0, B) or child == parent (nothing happens).
+ * reserve  rows grow to new_lens[b] (a shorter one leaves the row as it is), with free pages for the positions that need them.  granted[b]
+ *          (or NULL): 1, or 0 where the table or the pages left (after those of the rows before it) do not suffice; the row is then
+ *          as it was.  new_lens must not be seqlens itself.
+ * compact  with L pages in use, the i-th page in use at or behind page L moves to the i-th free page in front of it: contents,
+ *          refs and the rows' entries.  Pages L .. are free afterwards; *live (device, or NULL) = L.
+ */
+int amla_pages_workspace_size(int num_blocks, int B, size_t* bytes_out);
+int amla_pages_copy(void* cache, long long page_bytes, int num_blocks, const int32_t* src, const int32_t* dst, int n, void* cuda_stream);
+int amla_pages_free(int32_t* block_table, int32_t* seqlens, int32_t* refs, const int32_t* rows, int n, int B, int num_blocks,
+                    int max_blocks_per_seq, void* cuda_stream);
+int amla_pages_fork(void* cache, long long page_bytes, int32_t* block_table, int32_t* seqlens, int32_t* refs, const int32_t* parents,
+                    const int32_t* children, int n, int B, int num_blocks, int max_blocks_per_seq, int32_t* served, void* workspace,
+                    size_t workspace_bytes, void* cuda_stream);
+int amla_pages_reserve(int32_t* block_table, int32_t* seqlens, int32_t* refs, const int32_t* new_lens, int B, int num_blocks,
+                       int max_blocks_per_seq, int32_t* granted, void* workspace, size_t workspace_bytes, void* cuda_stream);
+int amla_pages_compact(void* cache, long long page_bytes, int32_t* block_table, const int32_t* seqlens, int32_t* refs, int B,
+                       int num_blocks, int max_blocks_per_seq, int32_t* live, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Synchronises `cuda_stream` and reads the status word the kernels keep at the start of the
  * workspace: AMLA_OK, or AMLA_ERR_DEVICE_TIMEOUT if a bounded wait inside a kernel expired (the
  * kernel then returned early and the outputs are undefined).  Optional. */

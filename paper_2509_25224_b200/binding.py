@@ -38,10 +38,13 @@ EXPORTS = [
     "amla_check_status", "amla_last_launch_count", "amla_plan_host", "amla_profile_enable",
     "amla_profile_last_ms", "amla_mla_decode_static", "amla_static_check_status", "amla_wait_selftest",
     "amla_last_item_rows", "amla_validate_paging_host", "amla_mla_decode_fp8", "amla_mla_decode_fp8_workspace_size",
+    "amla_mla_decode_fp4", "amla_mla_decode_fp4_workspace_size", "amla_cache_store_fp4", "amla_cache_load_fp4",
+    "amla_pages_workspace_size", "amla_pages_copy", "amla_pages_free", "amla_pages_fork", "amla_pages_reserve", "amla_pages_compact",
 ]
 
 _lib = None
 _PAGE_SHAPE = (64, 576)
+_FP4_PAGE_SHAPE = (64 * (576 // 2 + 576 // 16),)      # 64 rows of E2M1 pairs, then 64 rows of E4M3 scales
 
 
 class AmlaError(RuntimeError):
@@ -72,6 +75,27 @@ def lib() -> ctypes.CDLL:
         L.amla_mla_decode_fp8_workspace_size.restype = i32
         L.amla_mla_decode_fp8.argtypes = [vp, vp, f32, vp, vp, f32, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp, i32]
         L.amla_mla_decode_fp8.restype = i32
+        L.amla_mla_decode_fp4_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+        L.amla_mla_decode_fp4_workspace_size.restype = i32
+        L.amla_mla_decode_fp4.argtypes = [vp, vp, f32, vp, vp, f32, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.amla_mla_decode_fp4.restype = i32
+        i64 = ctypes.c_longlong
+        L.amla_cache_store_fp4.argtypes = [vp, i64, i32, vp, vp, f32, vp, vp, i32, i32, i32, vp]
+        L.amla_cache_store_fp4.restype = i32
+        L.amla_cache_load_fp4.argtypes = [vp, f32, vp, vp, vp, i32, i32, i32, vp, i64, i32, vp]
+        L.amla_cache_load_fp4.restype = i32
+        L.amla_pages_workspace_size.argtypes = [i32, i32, ctypes.POINTER(sz)]
+        L.amla_pages_workspace_size.restype = i32
+        L.amla_pages_copy.argtypes = [vp, i64, i32, vp, vp, i32, vp]
+        L.amla_pages_copy.restype = i32
+        L.amla_pages_free.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
+        L.amla_pages_free.restype = i32
+        L.amla_pages_fork.argtypes = [vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, sz, vp]
+        L.amla_pages_fork.restype = i32
+        L.amla_pages_reserve.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+        L.amla_pages_reserve.restype = i32
+        L.amla_pages_compact.argtypes = [vp, i64, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+        L.amla_pages_compact.restype = i32
         L.amla_mla_decode_static.argtypes = [vp, vp, vp, vp, f32, i32, i32, i32, i32, i32, vp, vp, vp]
         L.amla_mla_decode_static.restype = i32
         L.amla_static_check_status.argtypes = [vp]
@@ -186,6 +210,50 @@ def mla_decode_fp8(q, kv_cache_e4m3, kv_scale: float, block_table, seqlens, soft
                (q.data_ptr(), kv_cache_e4m3.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), float(softmax_scale), B, Sq, H,
                 kv_cache_e4m3.shape[0], block_table.shape[1], out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.numel()),
                (DEFAULT_FLAGS if flags is None else int(flags),), "amla_mla_decode_fp8")
+    return out, lse
+
+
+def fp4_workspace_size(B: int, Sq: int, H: int, max_blocks_per_seq: int, device: int = 0) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().amla_mla_decode_fp4_workspace_size(B, Sq, H, max_blocks_per_seq, device or 0, ctypes.byref(n))
+    if rc != AMLA_OK:
+        raise AmlaError(rc, "amla_mla_decode_fp4_workspace_size")
+    return int(n.value)
+
+
+def mla_decode_fp4(q, kv_cache_fp4, kv_scale: float, block_table, seqlens, softmax_scale: float, out=None, lse=None, workspace=None):
+    """amla_mla_decode_fp4 on device tensors: q bf16 [B,Sq,H,576], kv_cache_fp4 uint8 [num_blocks,20736] (E2M1 numbers and their E4M3
+    scales, as paging.cache_store_fp4 writes them; element value = e2m1 * e4m3 * kv_scale).  Returns (out bf16, lse fp32)."""
+    import torch
+
+    if kv_cache_fp4.dtype is not torch.uint8 or q.dtype is not torch.bfloat16:
+        raise ValueError("q must be bfloat16 and the cache uint8 (4-bit pages)")
+    if block_table.dtype is not torch.int32 or seqlens.dtype is not torch.int32:
+        raise ValueError("block_table and seqlens must be int32")
+    if not (q.is_contiguous() and kv_cache_fp4.is_contiguous() and block_table.is_contiguous() and seqlens.is_contiguous()):
+        raise ValueError("inputs must be contiguous")
+    B, Sq, H, d = q.shape
+    if d != 576 or kv_cache_fp4.shape[1:] != _FP4_PAGE_SHAPE or block_table.shape[0] != B or seqlens.shape[0] != B:
+        raise ValueError("shape mismatch")
+    dev = q.device
+    if kv_cache_fp4.device != dev or block_table.device != dev or seqlens.device != dev:
+        raise ValueError("inputs must be on one device")
+    if _lib is None:
+        lib()
+    if out is None:
+        out = torch.empty((B, Sq, H, 512), dtype=torch.bfloat16, device=dev)
+    elif out.dtype is not torch.bfloat16 or out.shape != (B, Sq, H, 512) or not out.is_contiguous() or out.device != dev:
+        raise ValueError("out must be a contiguous bfloat16 [B,Sq,H,512] on the inputs' device")
+    if lse is None:
+        lse = torch.empty((B, Sq, H), dtype=torch.float32, device=dev)
+    elif lse.dtype is not torch.float32 or lse.shape != (B, Sq, H) or not lse.is_contiguous() or lse.device != dev:
+        raise ValueError("lse must be a contiguous float32 [B,Sq,H] on the inputs' device")
+    if workspace is None:
+        workspace = torch.empty(fp4_workspace_size(B, Sq, H, block_table.shape[1], dev.index or 0), dtype=torch.uint8, device=dev)
+    _on_device(dev, _lib.amla_mla_decode_fp4,
+               (q.data_ptr(), kv_cache_fp4.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), float(softmax_scale), B, Sq, H,
+                kv_cache_fp4.shape[0], block_table.shape[1], out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size()),
+               (), "amla_mla_decode_fp4")
     return out, lse
 
 

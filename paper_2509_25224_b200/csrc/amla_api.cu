@@ -7,6 +7,7 @@
 
 #include "../../include/amla.h"
 #include "amla_common.cuh"
+#include "amla_fp4.cuh"
 
 namespace amla {
 cudaError_t launch_plan(const DecodeParams& prm, int* prefix_out, cudaStream_t stream);
@@ -19,6 +20,8 @@ cudaError_t launch_decode_quad(const DecodeParams& prm, cudaStream_t stream, int
 cudaError_t launch_wait_selftest(int* status, unsigned long long limit_ns, cudaStream_t stream);
 cudaError_t launch_widen_pages(const uint8_t* kv8, const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks,
                                int max_blocks_per_seq, __nv_bfloat16* scratch, int32_t* table_out, cudaStream_t stream);
+cudaError_t launch_widen_pages4(const uint8_t* cache, const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks, int max_blocks_per_seq, __nv_bfloat16* scratch,
+                                int32_t* table_out, cudaStream_t stream);
 int decode_pair_parts(int sm_count);
 int decode_quad_parts(int device, int sm_count);
 
@@ -350,6 +353,37 @@ extern "C" int amla_mla_decode_fp8(const void* q, const void* kv_cache_e4m3, flo
   ++g_last_launches;
   return decode_impl(q, pages, nullptr, table2, seqlens, softmax_scale * kv_scale, kv_scale, B, Sq, H, B * max_blocks_per_seq,
                      max_blocks_per_seq, out, lse, workspace, base, cuda_stream, flags);
+}
+
+extern "C" int amla_mla_decode_fp4_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int device, size_t* bytes_out) {
+  return amla_mla_decode_fp8_workspace_size(B, Sq, H, max_blocks_per_seq, device, bytes_out);
+}
+
+extern "C" int amla_mla_decode_fp4(const void* q, const void* kv_cache_fp4, float kv_scale, const int32_t* block_table, const int32_t* seqlens, float softmax_scale, int B, int Sq,
+                                   int H, int num_blocks, int max_blocks_per_seq, void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  g_last_launches = 0;
+  const int flags = AMLA_RESCALE_ALG2 | AMLA_LAZY(AMLA_DEFAULT_TAU);
+  int rc = check_arguments(q, kv_cache_fp4, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks, max_blocks_per_seq, out, lse, workspace, flags);
+  if (rc != AMLA_OK) return rc;
+  if (!fp4_scale_ok(kv_scale)) return AMLA_ERR_INVALID_ARG;
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); return AMLA_ERR_CUDA; }
+  size_t base = 0;
+  rc = amla_mla_decode_workspace_size(B, Sq, H, max_blocks_per_seq, device, &base);
+  if (rc != AMLA_OK) return rc;
+  base = align_up(base);
+  const size_t tbytes = fp8_table_bytes(B, max_blocks_per_seq), pbytes = fp8_pages_bytes(B, max_blocks_per_seq);
+  if (workspace_bytes < base + tbytes + pbytes) return AMLA_ERR_WORKSPACE;
+  if (static_cast<long long>(B) * max_blocks_per_seq > (1ll << 30)) return AMLA_ERR_UNSUPPORTED;
+  char* ws = static_cast<char*>(workspace);
+  int32_t* table2 = reinterpret_cast<int32_t*>(ws + base);
+  __nv_bfloat16* pages = reinterpret_cast<__nv_bfloat16*>(ws + base + tbytes);
+  if (launch_widen_pages4(static_cast<const uint8_t*>(kv_cache_fp4), block_table, seqlens, B, num_blocks, max_blocks_per_seq, pages, table2, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) {
+    cudaGetLastError();
+    return AMLA_ERR_CUDA;
+  }
+  ++g_last_launches;
+  return decode_impl(q, pages, nullptr, table2, seqlens, softmax_scale * kv_scale, kv_scale, B, Sq, H, B * max_blocks_per_seq, max_blocks_per_seq, out, lse, workspace, base, cuda_stream, flags);
 }
 
 extern "C" int amla_mla_decode(const void* q, const void* kv_cache, const int32_t* block_table,
