@@ -179,7 +179,8 @@ int amla_mla_decode_fp8(const void* q, const void* kv_cache_e4m3, float kv_scale
  *   kv_scale       one factor for the whole cache, 2^-100 .. 2^100
  *   workspace      at least amla_mla_decode_fp4_workspace_size() bytes, 256-byte aligned
  *
- * A call reads 324 bytes a key (bf16: 1152).  Rows of a used page beyond the sequence length may hold anything.  A block-table entry outside [0, num_blocks) of a used page reads
+ * A call reads 324 bytes a key (bf16: 1152).  Rows of a used page beyond the sequence length may hold anything.  A scale that is
+ * a NaN makes the rows that see the key NaN.  A block-table entry outside [0, num_blocks) of a used page reads
  * as a page of zeros.  Everything else (visibility rule, outputs, shapes, errors) is as for amla_mla_decode; amla_check_status reads the status.
  */
 int amla_mla_decode_fp4_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int device, size_t* bytes_out);

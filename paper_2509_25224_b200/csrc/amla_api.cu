@@ -20,8 +20,8 @@ cudaError_t launch_decode_quad(const DecodeParams& prm, cudaStream_t stream, int
 cudaError_t launch_wait_selftest(int* status, unsigned long long limit_ns, cudaStream_t stream);
 cudaError_t launch_widen_pages(const uint8_t* kv8, const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks,
                                int max_blocks_per_seq, __nv_bfloat16* scratch, int32_t* table_out, cudaStream_t stream);
-cudaError_t launch_widen_pages4(const uint8_t* cache, const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks, int max_blocks_per_seq, __nv_bfloat16* scratch,
-                                int32_t* table_out, cudaStream_t stream);
+cudaError_t launch_decode_fp4(const DecodeParams& prm, cudaStream_t stream);
+int fp4_item_rows(int rows);
 int decode_pair_parts(int sm_count);
 int decode_quad_parts(int device, int sm_count);
 
@@ -45,6 +45,17 @@ Layout make_layout(int n_items, int max_parts) {
   l.part_o_off = l.part_lse_off + align_up(sizeof(float) * 2 * static_cast<size_t>(max_parts) * kRowBlock);
   l.total = l.part_o_off + sizeof(float) * 2 * static_cast<size_t>(max_parts) * kRowBlock * kDv;
   return l;
+}
+
+// Sets what of prm lies in the workspace; returns the schedule prefix.
+int* carve(DecodeParams& prm, char* ws, const Layout& lay) {
+  int* prefix = reinterpret_cast<int*>(ws + lay.prefix_off);
+  prm.status = reinterpret_cast<int*>(ws + lay.status_off);
+  prm.prefix = prefix;
+  prm.merge_info = reinterpret_cast<int4*>(ws + lay.merge_off);
+  prm.part_lse = reinterpret_cast<float*>(ws + lay.part_lse_off);
+  prm.part_o = reinterpret_cast<float*>(ws + lay.part_o_off);
+  return prefix;
 }
 
 int check_shape(int B, int Sq, int H, int max_blocks_per_seq) {
@@ -111,6 +122,17 @@ static bool blocks_of_256(const DecodeParams& prm, int pair_parts, int quad_part
   return 21.5 + 2.08 * items2 * tiles + 11. * std::max(items2 - 1., 0.) < 13. + 1.41 * items1 * pages + 6. * items1;
 }
 
+// No more parts than the longest schedule that the block table's width allows can fill.  A schedule of one score tile at
+// most is one part: nothing is split and no combine kernel runs.
+static void cap_parts(DecodeParams& prm) {
+  const long long tiles = (static_cast<long long>(prm.max_blocks_per_seq) * kPage + prm.tile_keys - 1) / prm.tile_keys;
+  const long long longest = prm.n_items * tiles + (prm.n_items - 1ll) * prm.ovh;
+  if (longest * prm.tile_keys <= 256) prm.P = 1;
+  else prm.P = static_cast<int>(std::min<long long>(prm.P, (longest + prm.min_share - 1) / prm.min_share));
+  // (a plan made in the decode kernel may begin as a guess: any lengths that the table has room for must add up)
+  prm.fused_plan = prm.n_items <= kFusedPlanMaxItems && longest <= 0x7fffffff ? 1 : 0;
+}
+
 // Chooses the kernel for the shape and fills the schedule fields of prm (rows per item, keys per tile, parts):
 //   up to 32 query rows of a bf16 cache      the kernel for few rows
 //   more than 128 rows of a bf16 cache       the 256-row kernel (four-CTA clusters, pair MMAs) where it is the faster one
@@ -138,16 +160,7 @@ int configure_schedule(DecodeParams& prm, int device, int sms, int flags) {
   prm.nrb = (prm.R + prm.item_rows - 1) / prm.item_rows;
   prm.n_items = prm.B * prm.nrb;
   prm.P = simt || few ? sms : quad ? quad_parts : decode_pair_parts(sms);
-  // No more parts than the longest schedule that the block table's width allows can fill.  A schedule of one score tile at
-  // most is one part: nothing is split and no combine kernel runs.
-  const long long tiles = (static_cast<long long>(prm.max_blocks_per_seq) * kPage + prm.tile_keys - 1) / prm.tile_keys;
-  const long long longest = prm.n_items * tiles + (prm.n_items - 1ll) * prm.ovh;
-  if (!simt) {
-    if (longest * prm.tile_keys <= 256) prm.P = 1;
-    else prm.P = static_cast<int>(std::min<long long>(prm.P, (longest + prm.min_share - 1) / prm.min_share));
-  }
-  // (a plan made in the decode kernel may begin as a guess: any lengths that the table has room for must add up)
-  prm.fused_plan = (!simt && prm.n_items <= kFusedPlanMaxItems && longest <= 0x7fffffff) ? 1 : 0;
+  if (simt) prm.fused_plan = 0; else cap_parts(prm);
   return AMLA_OK;
 }
 
@@ -165,7 +178,8 @@ int launch_decode_call(const DecodeParams& prm, int* prefix, cudaStream_t stream
     if (launch_decode_simt(prm, stream) != cudaSuccess) { cudaGetLastError(); return AMLA_ERR_CUDA; }
   } else {
     int unsupported = 0;
-    const cudaError_t err = prm.item_rows > kRowBlock   ? launch_decode_quad(prm, stream, &unsupported)
+    const cudaError_t err = prm.kv4 != nullptr          ? launch_decode_fp4(prm, stream)
+                            : prm.item_rows > kRowBlock ? launch_decode_quad(prm, stream, &unsupported)
                             : prm.item_rows < kRowBlock ? launch_decode_few(prm, stream, &unsupported)
                                                         : launch_decode_pair(prm, stream, &unsupported);
     if (err != cudaSuccess) {
@@ -250,9 +264,9 @@ int decode_impl(const void* q, const void* kv_cache, const uint8_t* kv8, const i
   const Layout lay = make_layout(B * ((Sq * H + kRowBlock - 1) / kRowBlock), sms);
   if (workspace_bytes < lay.total) return AMLA_ERR_WORKSPACE;
 
-  char* ws = static_cast<char*>(workspace);
   DecodeParams prm;
   std::memset(&prm, 0, sizeof(prm));
+  int* prefix = carve(prm, static_cast<char*>(workspace), lay);
   prm.q = static_cast<const __nv_bfloat16*>(q);
   prm.kv = static_cast<const __nv_bfloat16*>(kv_cache);
   prm.kv8 = kv8;
@@ -260,12 +274,6 @@ int decode_impl(const void* q, const void* kv_cache, const uint8_t* kv8, const i
   prm.seqlens = seqlens;
   prm.out = static_cast<__nv_bfloat16*>(out);
   prm.lse = lse;
-  prm.status = reinterpret_cast<int*>(ws + lay.status_off);
-  int* prefix = reinterpret_cast<int*>(ws + lay.prefix_off);
-  prm.prefix = prefix;
-  prm.merge_info = reinterpret_cast<int4*>(ws + lay.merge_off);
-  prm.part_lse = reinterpret_cast<float*>(ws + lay.part_lse_off);
-  prm.part_o = reinterpret_cast<float*>(ws + lay.part_o_off);
   prm.scale_log2 = softmax_scale * kLog2e;
   prm.out_scale = out_scale;
   prm.B = B; prm.Sq = Sq; prm.H = H;
@@ -355,35 +363,62 @@ extern "C" int amla_mla_decode_fp8(const void* q, const void* kv_cache_e4m3, flo
                      max_blocks_per_seq, out, lse, workspace, base, cuda_stream, flags);
 }
 
+// (A block of 16, 32 or 64 rows is an item: more of them than of 128 rows, and partials no larger.)
 extern "C" int amla_mla_decode_fp4_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int device, size_t* bytes_out) {
-  return amla_mla_decode_fp8_workspace_size(B, Sq, H, max_blocks_per_seq, device, bytes_out);
+  if (!bytes_out) return AMLA_ERR_INVALID_ARG;
+  int rc = check_shape(B, Sq, H, max_blocks_per_seq);
+  if (rc != AMLA_OK) return rc;
+  const int item_rows = fp4_item_rows(Sq * H), nrb = (Sq * H + item_rows - 1) / item_rows;
+  if (static_cast<long long>(B) * nrb > (1ll << 24)) return AMLA_ERR_UNSUPPORTED;
+  int sms = 0, cc = 0;
+  rc = sm_count_of(device, &sms, &cc);
+  if (rc != AMLA_OK) return rc;
+  *bytes_out = make_layout(B * nrb, sms).total;
+  return AMLA_OK;
 }
 
 extern "C" int amla_mla_decode_fp4(const void* q, const void* kv_cache_fp4, float kv_scale, const int32_t* block_table, const int32_t* seqlens, float softmax_scale, int B, int Sq,
                                    int H, int num_blocks, int max_blocks_per_seq, void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   g_last_launches = 0;
-  const int flags = AMLA_RESCALE_ALG2 | AMLA_LAZY(AMLA_DEFAULT_TAU);
-  int rc = check_arguments(q, kv_cache_fp4, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks, max_blocks_per_seq, out, lse, workspace, flags);
+  int rc = check_arguments(q, kv_cache_fp4, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks, max_blocks_per_seq, out, lse, workspace, 0);
   if (rc != AMLA_OK) return rc;
   if (!fp4_scale_ok(kv_scale)) return AMLA_ERR_INVALID_ARG;
+  const int item_rows = fp4_item_rows(Sq * H), nrb = (Sq * H + item_rows - 1) / item_rows;
+  if (static_cast<long long>(B) * nrb > (1ll << 24)) return AMLA_ERR_UNSUPPORTED;
   int device = 0;
   if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); return AMLA_ERR_CUDA; }
-  size_t base = 0;
-  rc = amla_mla_decode_workspace_size(B, Sq, H, max_blocks_per_seq, device, &base);
+  int sms = 0, cc = 0;
+  rc = sm_count_of(device, &sms, &cc);
   if (rc != AMLA_OK) return rc;
-  base = align_up(base);
-  const size_t tbytes = fp8_table_bytes(B, max_blocks_per_seq), pbytes = fp8_pages_bytes(B, max_blocks_per_seq);
-  if (workspace_bytes < base + tbytes + pbytes) return AMLA_ERR_WORKSPACE;
-  if (static_cast<long long>(B) * max_blocks_per_seq > (1ll << 30)) return AMLA_ERR_UNSUPPORTED;
-  char* ws = static_cast<char*>(workspace);
-  int32_t* table2 = reinterpret_cast<int32_t*>(ws + base);
-  __nv_bfloat16* pages = reinterpret_cast<__nv_bfloat16*>(ws + base + tbytes);
-  if (launch_widen_pages4(static_cast<const uint8_t*>(kv_cache_fp4), block_table, seqlens, B, num_blocks, max_blocks_per_seq, pages, table2, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) {
-    cudaGetLastError();
-    return AMLA_ERR_CUDA;
-  }
-  ++g_last_launches;
-  return decode_impl(q, pages, nullptr, table2, seqlens, softmax_scale * kv_scale, kv_scale, B, Sq, H, B * max_blocks_per_seq, max_blocks_per_seq, out, lse, workspace, base, cuda_stream, flags);
+  if (cc != 10) return AMLA_ERR_UNSUPPORTED;
+  const Layout lay = make_layout(B * nrb, sms);
+  if (workspace_bytes < lay.total) return AMLA_ERR_WORKSPACE;
+
+  DecodeParams prm;
+  std::memset(&prm, 0, sizeof(prm));
+  int* prefix = carve(prm, static_cast<char*>(workspace), lay);
+  prm.q = static_cast<const __nv_bfloat16*>(q);
+  prm.kv4 = static_cast<const uint8_t*>(kv_cache_fp4);
+  prm.block_table = block_table;
+  prm.seqlens = seqlens;
+  prm.out = static_cast<__nv_bfloat16*>(out);
+  prm.lse = lse;
+  prm.scale_log2 = softmax_scale * kv_scale * kLog2e;      // logits: scale * q . (k * kv_scale); output: sum p * (v * kv_scale)
+  prm.out_scale = kv_scale;
+  prm.B = B; prm.Sq = Sq; prm.H = H;
+  prm.R = Sq * H;
+  prm.num_blocks = num_blocks;
+  prm.max_blocks_per_seq = max_blocks_per_seq;
+  prm.sms = sms;
+  prm.item_rows = item_rows;
+  prm.nrb = nrb;
+  prm.n_items = B * nrb;
+  prm.tile_keys = kPage;
+  prm.ovh = kFp4OverheadTiles;
+  prm.min_share = kMinPartKeys / kPage;
+  prm.P = sms;
+  cap_parts(prm);
+  return launch_decode_call(prm, prefix, static_cast<cudaStream_t>(cuda_stream), &g_last_launches, profile_mark);
 }
 
 extern "C" int amla_mla_decode(const void* q, const void* kv_cache, const int32_t* block_table,

@@ -24,6 +24,7 @@ struct DecodeParams {
   const __nv_bfloat16* q;        // [B, Sq, H, 576] == [B, R, 576]
   const __nv_bfloat16* kv;       // [num_blocks, 64, 576]
   const uint8_t* kv8;            // an E4M3 cache [num_blocks, 64, 576] instead of kv (or nullptr)
+  const uint8_t* kv4;            // a 4-bit cache [num_blocks, 20736] instead of kv (or nullptr)
   const int32_t* block_table;    // [B, max_blocks_per_seq]
   const int32_t* seqlens;        // [B]
   __nv_bfloat16* out;            // [B, R, 512]
@@ -49,7 +50,7 @@ struct DecodeParams {
   int fused_plan;                // the decode kernel computes `prefix` itself (few items), no schedule kernel
   int flags;
   int tile_keys;                 // keys per schedule tile: 64 (one page) or 128 (two pages, the 256-row kernel)
-  int item_rows;                 // query rows per work item: 32, 128 or 256, after the kernel (nrb counts these)
+  int item_rows;                 // query rows per work item, after the kernel (nrb counts these): 32, 128 or 256; 4-bit cache 16, 32 or 64
   int ovh;                       // schedule positions that stand for the cost of starting an item
   int min_share;                 // a part is given at least this many positions
   unsigned long long* trace;     // timeline buffer of a -DAMLA_TRACE build, else unused (nullptr)
@@ -91,6 +92,10 @@ constexpr int kQuadOverheadTiles = AMLA_QUAD_OVERHEAD_TILES;
 #define AMLA_FEW_OVERHEAD_TILES 3             // kernel for few rows: in 64-key pages (a build-time knob; 2-4 measure alike, 1 and 6 worse)
 #endif
 constexpr int kFewOverheadTiles = AMLA_FEW_OVERHEAD_TILES;
+#ifndef AMLA_FP4_OVERHEAD_TILES
+#define AMLA_FP4_OVERHEAD_TILES 4             // kernel for a 4-bit cache: in 64-key pages
+#endif
+constexpr int kFp4OverheadTiles = AMLA_FP4_OVERHEAD_TILES;
 constexpr int kMinPartKeys = 128;           // a part holds at least this many keys: a shorter one takes as long, and every part is a partial to merge
 constexpr int kFusedPlanMaxItems = 2048;   // up to this many items every decode CTA computes the prefix itself
 

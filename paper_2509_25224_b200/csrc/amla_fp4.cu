@@ -169,45 +169,6 @@ __global__ void __launch_bounds__(kThreads) load_fp4_kernel(const uint8_t* __res
   }
 }
 
-// Widens the pages that a batch uses into a bf16 cache, ahead of the bf16 kernels (without kv_scale, which is folded into the softmax
-// scale and the final normalisation).  One block per (sequence, page slot): slot i of sequence b becomes page b * max_blocks + i; a page
-// index outside the cache, and what is beyond the sequence's length, gives zeros.
-__global__ void __launch_bounds__(kThreads) widen_pages4_kernel(const uint8_t* __restrict__ cache, const int32_t* __restrict__ block_table, const int32_t* __restrict__ seqlens, int num_blocks,
-                                                                int max_blocks_per_seq, __nv_bfloat16* __restrict__ scratch, int32_t* __restrict__ table_out) {
-  asm volatile("griddepcontrol.launch_dependents;");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int b = blockIdx.x / max_blocks_per_seq, i = blockIdx.x % max_blocks_per_seq;
-  if (threadIdx.x == 0) table_out[blockIdx.x] = blockIdx.x;
-  const int n = min(max(seqlens[b], 0), max_blocks_per_seq * kPage);
-  if (i * kPage >= n) return;
-  const int32_t page = block_table[blockIdx.x];
-  const bool there = page >= 0 && page < num_blocks;
-  const uint8_t* src = cache + static_cast<size_t>(there ? page : 0) * kPageBytes4;
-  uint4* dst = reinterpret_cast<uint4*>(scratch + static_cast<size_t>(blockIdx.x) * kPage * kDqk);
-  for (int c = threadIdx.x; c < kPage * kTokenThreads; c += kThreads) {
-    const int row = c / kTokenThreads, col = c - row * kTokenThreads;
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (there && i * kPage + row < n) {
-      const uint32_t byte = src[kCodeBytes + row * kScaleRow + col / 2];
-      uint32_t h[4];
-      e2m1x8_to_f16x2(*reinterpret_cast<const uint32_t*>(src + row * kCodeRow + 4 * col), h);
-      const uint32_t s2 = e4m3x2_to_f16x2(byte | (byte << 8));
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 f = unpack_f16x2(mul_f16x2(h[k], s2));
-        w[k] = sm100::pack_bf16x2(f.x, f.y);
-      }
-    }
-    dst[c] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
-
-cudaError_t launch_widen_pages4(const uint8_t* cache, const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks, int max_blocks_per_seq, __nv_bfloat16* scratch,
-                                int32_t* table_out, cudaStream_t stream) {
-  widen_pages4_kernel<<<B * max_blocks_per_seq, kThreads, 0, stream>>>(cache, block_table, seqlens, num_blocks, max_blocks_per_seq, scratch, table_out);
-  return cudaGetLastError();
-}
-
 namespace {
 
 template <typename... Args>

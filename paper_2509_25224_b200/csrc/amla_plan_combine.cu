@@ -65,6 +65,12 @@ __global__ void plan_kernel(const int32_t* __restrict__ seqlens, int nrb, int n_
 // 192 sequences of 1-512 keys 45.4 -> 44.2; 32 of 1-8 K with 16 rows 37.5 -> 36.4; 96 of 2048 73.1 -> 71.7 cool.
 // (One block per SM that walks over the rows and fits beside a decode CTA lets the next call's decode kernel in at once, but
 // takes 10 us where these take 4: 32 x 4096 keys 55.8 -> 61.5.)
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 template <bool kFloat, int kCols, int kSplitWarps>
 __global__ void __launch_bounds__(128, kCols == 16 ? 7 : kCols == 8 ? 8 : 5) combine_kernel(const __grid_constant__ DecodeParams prm) {
   // A decode kernel that follows on the stream may set itself up beside this kernel (it writes nothing this kernel
@@ -132,10 +138,10 @@ __global__ void __launch_bounds__(128, kCols == 16 ? 7 : kCols == 8 ? 8 : 5) com
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) x[k] = fetch(min(k, nsplit - 1));
   }
-  float mx = ls;
-  for (int s = lane + 32; s < nsplit; s += 32) mx = fmaxf(mx, prm.part_lse[part_row(s)]);
+  float mx = ls;                                           // (a partial whose lse is a NaN makes the row one)
+  for (int s = lane + 32; s < nsplit; s += 32) mx = max_nan(mx, prm.part_lse[part_row(s)]);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  for (int o = 16; o; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   if (mx != -INFINITY) {                                   // else no split saw a visible key for this row: zeros
     ls = expf(ls - mx);                                    // 0 for a split that saw nothing
     if (nsplit <= kFast) {
@@ -167,7 +173,7 @@ __global__ void __launch_bounds__(128, kCols == 16 ? 7 : kCols == 8 ? 8 : 5) com
     __syncthreads();
     if (sw != 0) return;
 #pragma unroll
-    for (int k = 1; k < kSplitWarps; ++k) mx = fmaxf(mx, s_lse[k].x);
+    for (int k = 1; k < kSplitWarps; ++k) mx = max_nan(mx, s_lse[k].x);
     acc[0] = acc[1] = acc[2] = acc[3] = tot = 0.f;
     if (mx != -INFINITY) {
 #pragma unroll
@@ -179,7 +185,7 @@ __global__ void __launch_bounds__(128, kCols == 16 ? 7 : kCols == 8 ? 8 : 5) com
       }
     }
   }
-  const float inv = tot > 0.f ? 1.f / tot : 0.f;
+  const float inv = tot == 0.f ? 0.f : 1.f / tot;
   uint32_t pk[kCols / 2];
 #pragma unroll
   for (int i = 0; i < kCols / 2; ++i) {
@@ -193,7 +199,7 @@ __global__ void __launch_bounds__(128, kCols == 16 ? 7 : kCols == 8 ? 8 : 5) com
 #pragma unroll
     for (int i = 0; i < kCols / 8; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
   }
-  if (lane == 0 && col == 0) prm.lse[static_cast<size_t>(b) * prm.R + rin] = tot > 0.f ? mx + logf(tot) : -INFINITY;
+  if (lane == 0 && col == 0) prm.lse[static_cast<size_t>(b) * prm.R + rin] = tot == 0.f ? -INFINITY : mx + logf(tot);
 }
 
 cudaError_t launch_plan(const DecodeParams& prm, int* prefix_out, cudaStream_t stream) {
@@ -202,7 +208,7 @@ cudaError_t launch_plan(const DecodeParams& prm, int* prefix_out, cudaStream_t s
 }
 
 cudaError_t launch_combine(const DecodeParams& prm, cudaStream_t stream) {
-  const bool fp32 = prm.item_rows < kRowBlock;
+  const bool fp32 = prm.item_rows < kRowBlock && prm.kv4 == nullptr;
   const int rows = merge_groups(prm) * merge_rows(prm);
   const bool few = rows <= 8 * prm.sms;
   const int units = rows * (few ? 4 : fp32 ? 2 : 1);

@@ -8,6 +8,12 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+// What is executed seldom is kept out of line, but in a kernel that moves registers between its warpgroups (setmaxnreg), where the
+// compiler cannot place calls: such a source file defines this as __forceinline__ ahead of its includes.
+#ifndef AMLA_SELDOM
+#define AMLA_SELDOM __noinline__
+#endif
+
 namespace amla {
 namespace sm100 {
 
@@ -98,7 +104,7 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;   // 2 s: far beyond any legiti
 // Slow path of a wait, kept out of line so that the many call sites stay small (the role loops are
 // executed by single warps and are sensitive to instruction-cache footprint).
 template <bool kClusterAcquire>
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+__device__ AMLA_SELDOM bool mbar_wait_slow(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
   const uint64_t t0 = global_timer_ns();
   while (true) {
     for (int i = 0; i < 256; ++i) {
@@ -190,6 +196,10 @@ __device__ __forceinline__ void tma_load_3d_pair_hint(uint32_t dst_smem, const v
       "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;"
       ::"r"(dst_smem), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(cluster_bar), "l"(policy)
       : "memory");
+}
+// Contiguous global memory -> this CTA's shared memory (both 16-byte aligned, a multiple of 16 bytes); counted in bytes on `bar`.
+__device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst_smem), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 // Brings contiguous global memory into L2 (16-byte aligned, a multiple of 16 bytes).
 __device__ __forceinline__ void bulk_prefetch_l2(const void* p, uint32_t bytes) {

@@ -42,7 +42,7 @@ struct UnitFound {
   Unit u;
   int g;                           // position behind the unit
 };
-static __device__ __noinline__ UnitFound find_unit(const int* prefix, const int* seqlens, int n_items, int nrb, int item_rows, int max_keys, int ovh, int g, int g1) {
+static __device__ AMLA_SELDOM UnitFound find_unit(const int* prefix, const int* seqlens, int n_items, int nrb, int item_rows, int max_keys, int ovh, int g, int g1) {
   UnitFound f;
   f.u.t0 = f.u.t1 = 0;
   f.u.it = f.u.b = f.u.r0 = f.u.n_b = 0;
@@ -214,7 +214,7 @@ struct UnitIter {
 // Items without tiles have no unit: their output is zero and their lse -inf.  `who` of `step` writers takes every step-th
 // item; within an item this writes rows [row0, row0 + nrows) of its block.
 // (The function takes values: a reference would make every caller keep the kernel's parameters in local memory.)
-static __device__ __noinline__ void write_empty_items_of(const int* prefix, int n_items, int nrb, int item_rows, int R, __nv_bfloat16* out, float* lse,
+static __device__ AMLA_SELDOM void write_empty_items_of(const int* prefix, int n_items, int nrb, int item_rows, int R, __nv_bfloat16* out, float* lse,
                                                          int4* merge_info, int who, int step, int row0, int nrows, int tid, int threads) {
   for (int it = who; it < n_items; it += step) {
     if (prefix[it + 1] > prefix[it]) continue;

@@ -104,6 +104,13 @@ def test_decode_many_short_sequences(B, H):
     check(lens, 1, H)
 
 
+@pytest.mark.parametrize("H", [16, 32, 64, 128])
+def test_decode_units_of_many_tiles_behind_one_another(H):
+    # every part gets several units, of one tile to dozens: whoever runs ahead of whom at their ends has to come out right
+    lens = [int(n) for n in np.random.default_rng(H).integers(0, 1500, 260)]
+    check(lens, 1, H)
+
+
 @pytest.mark.parametrize("kv_scale", [1.0, 2.0 ** -20, 2.0 ** 20, 0.3])
 def test_decode_with_other_factors(kv_scale):
     w = workload([500, 77], 1, 128, kv_scale=kv_scale)
@@ -130,6 +137,24 @@ def test_decode_with_a_negative_scale():
     w = workload([700, 65, 1], 2, 64)
     out, lse = run(*w, 0.25, -SCALE)
     compare(out, lse, *expected(*w, 0.25, -SCALE))
+
+
+@pytest.mark.parametrize("H", [16, 64, 128])
+def test_what_is_not_a_number_stays_with_the_rows_that_see_it(H):
+    q, cache, table, lens = workload([200, 200, 200], 2, H)
+    q = q.copy()
+    q[0, 0, 3, 100] = 0x7FC0                                  # NaN in one row of Q
+    codes, scales = F.unpack(cache)
+    scales = scales.copy()
+    scales[table[1, 3], 199 - 192, 2] = 0x7F                  # NaN in the last key of sequence 1: seen by its last token alone
+    cache = F.pack(codes, scales)
+    out, lse = run(q, cache, table, lens, 0.25)
+    ref_out, ref_lse = expected(q, cache, table, lens, 0.25)
+    bad = np.zeros(lse.shape, bool)
+    bad[0, 0, 3] = True
+    bad[1, 1, :] = True
+    assert np.isnan(lse[bad]).all() and np.isnan(out[bad]).all()
+    compare(out[~bad], lse[~bad], ref_out[~bad], ref_lse[~bad])
 
 
 @pytest.mark.parametrize("beyond", [0, 100000, None])
