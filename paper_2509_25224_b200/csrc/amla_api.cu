@@ -413,6 +413,9 @@ extern "C" int amla_mla_decode_fp4(const void* q, const void* kv_cache_fp4, floa
   prm.item_rows = item_rows;
   prm.nrb = nrb;
   prm.n_items = B * nrb;
+#ifdef AMLA_TRACE
+  prm.trace = g_trace;
+#endif
   prm.tile_keys = kPage;
   prm.ovh = kFp4OverheadTiles;
   prm.min_share = kMinPartKeys / kPage;

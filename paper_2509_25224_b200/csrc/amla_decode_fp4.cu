@@ -20,9 +20,8 @@
 // next one comes when a key would exceed 2^15, and what f16 rounds to nothing is below 2^-33 of the reference.
 //
 // Warps 0-3: Q into f16, softmax (a thread is a key and has all rows; its share of the row sums stays in registers until the unit's
-// end), rescale, epilogue.  Warps 4-11: widening, two groups of four that take turns by chunk.  Warp 12 issues MMAs: Q K^T of the
-// next tile in front of P~V of this one, but for a unit's last tile, whose P~V comes first (the next unit's Q is on its way
-// meanwhile).  Warp 13 loads pages (bulk copies).
+// end), rescale, epilogue.  Warps 4-11 widen K and 12-19 V, four at a time by turns; warp 20 issues the products of K, 21
+// those of V; warp 22 loads pages (bulk copies).
 //
 // All waits are bounded; on expiry the kernel records kStatusTimeout and unwinds.
 #define AMLA_SELDOM __forceinline__
@@ -38,12 +37,10 @@ using namespace sm100;
 
 namespace {
 
-constexpr int kSoftmaxWarps = 4, kWidenWarps = 8;
-constexpr int kMmaWarp = 12, kLoadWarp = 13;
-constexpr int kThreads = 32 * 16;                        // (registers are given out by groups of four warps: 14, 15 have no role)
-// Registers a thread, by warpgroup: what the block is launched with is 512 threads x 128
-constexpr int kSoftmaxRegs = 232, kWidenRegs = 96, kIssueRegs = 80;
-static_assert(kSoftmaxRegs + 2 * kWidenRegs + kIssueRegs <= 4 * 128, "the block has no more to give out");
+constexpr int kSoftmaxWarps = 4, kWidenWarps = 16;      // K: two groups of four, V: two groups of four
+constexpr int kQkWarp = 20, kPvWarp = 21, kLoadWarp = 22;
+constexpr int kThreads = 32 * 24;                       // (registers are given out by groups of four warps: 23 has no role)
+constexpr int kLaunchRegs = 80;                         // a thread's at launch: 65536 / 768, rounded down to a multiple of 8
 constexpr int kColBlocks = kDqk / 64;                   // K chunks of a tile
 constexpr int kVChunks = 8;                             // V chunks of a tile: (2 halves of the columns) x (4 quarters of the keys)
 constexpr uint32_t kPBytes = 128 * 128;                 // P~: [128 keys][64 rows of f16], 128-byte swizzle
@@ -53,10 +50,15 @@ constexpr float kFar = 1e30f;                           // n of a row that has s
 
 template <int kN>
 struct Shape {
+  // Registers a thread, by warpgroup (softmax; four of widening; issue): together what the block is launched with
+  static constexpr int kSoftmaxRegs = kN == 64 ? 224 : 168, kWidenRegs = kN == 64 ? 48 : 64, kIssueRegs = kN == 64 ? 64 : 56;
+  static_assert(kSoftmaxRegs + 4 * kWidenRegs + kIssueRegs <= 6 * kLaunchRegs, "the block has no more to give out");
   static constexpr int kCols = kN < 32 ? kN : 32;       // rows that the softmax has in registers at a time
   static constexpr int kParts = kN / kCols;
   static constexpr int kSlots = kN == 64 ? 6 : kN == 32 ? 8 : 9;      // pages in shared memory
-  static constexpr int kBufs = kN == 64 ? 4 : 8;        // operand chunks in tensor memory
+  // Operand chunks in tensor memory, of K and of V: numbers that divide a tile's, so that a tile's chunks always have the same places.
+  static constexpr int kKBufs = 3, kVBufs = kN == 64 ? 2 : 4;
+  static constexpr int kSBufs = kN == 64 ? 1 : 2;       // score tiles in tensor memory
   static constexpr uint32_t kQBlock = kN * 128;         // [rows][64 columns of f16], 128-byte swizzle
   static constexpr uint32_t kOffP = kColBlocks * kQBlock;
   static constexpr uint32_t kOffRaw = kOffP + kPBytes;
@@ -75,36 +77,30 @@ struct Shape {
   static constexpr uint32_t kOffFirst = kOffLens + kSmemPlanItems * 4;
   static constexpr uint32_t kBytes = kOffFirst + sizeof(FirstUnit);
   // tensor-memory columns
-  static constexpr uint32_t kOCol = 0, kSCol = 4 * kN, kRing = 512 - 32 * kBufs;
-  enum { X_FULL = 0, X_EMPTY = X_FULL + kSlots, X_AFULL = X_EMPTY + kSlots, X_AEMPTY = X_AFULL + kBufs, X_QREADY = X_AEMPTY + kBufs, X_SFULL, X_SEMPTY = X_SFULL + 2, X_PREADY = X_SEMPTY + 2,
-         X_PVDONE, X_MOVES, X_MAX, X_SUMS, X_NUM };
+  static constexpr uint32_t kOCol = 0, kSCol = 4 * kN, kKCol = 512 - 32 * (kKBufs + kVBufs), kVCol = 512 - 32 * kVBufs;
+  enum { X_FULL = 0, X_EMPTY = X_FULL + kSlots, X_KFULL = X_EMPTY + kSlots, X_KEMPTY = X_KFULL + kKBufs, X_VFULL = X_KEMPTY + kKBufs, X_VEMPTY = X_VFULL + kVBufs, X_QREADY = X_VEMPTY + kVBufs,
+         X_SFULL, X_SEMPTY = X_SFULL + kSBufs, X_PREADY = X_SEMPTY + kSBufs, X_PVDONE, X_MOVES, X_MAX, X_SUMS, X_NUM };
   static_assert(X_NUM * 8 + 8 <= kBarBytes, "barrier area too small");
   static_assert(kBytes <= 232448, "exceeds the shared memory a block can opt in to");
   static_assert(kOffP % 1024 == 0 && kOffRaw % 1024 == 0 && kPageBytes4 % 16 == 0 && kOffBars % 8 == 0 && kOffMoves % 16 == 0 && kOffMult % 16 == 0, "alignment");
-  static_assert(kSCol + 2 * kN <= kRing && kSlots <= 12, "tensor memory");
+  static_assert(kSCol + kSBufs * kN <= kKCol && kSlots <= 12, "tensor memory");
+  static_assert(kColBlocks % kKBufs == 0 && kVChunks % kVBufs == 0 && (kVBufs == 2 || kVBufs == 4), "places of chunks");
 };
 
 __device__ __forceinline__ void report_timeout(int* status) { atomicExch(status, kStatusTimeout); }
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_inline(bar, parity)); }
 
 using Tiles = TileIter<2>;
 
 __device__ __forceinline__ float ld_shared_f32(uint32_t addr) { return __uint_as_float(ld_shared_b32(addr)); }
-__device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
-}
 __device__ __forceinline__ float warp_max(float v) {
   float r;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
-// 16 lanes x 16 columns: thread (g = lane / 4, q = lane % 4) gives columns 2q, 2q + 1 of lanes g (r0, r1) and g + 8 (r2, r3), then
-// the same of columns 8 ..
-__device__ __forceinline__ void tmem_st_16x256b_x2(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
+// 16 lanes x 8 columns: thread (g = lane / 4, q = lane % 4) gives columns 2q, 2q + 1 of lanes g (r0, r1) and g + 8 (r2, r3)
+__device__ __forceinline__ void tmem_st_16x256b_x1(uint32_t taddr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 template <int kCount>
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[kCount]) {
@@ -158,6 +154,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
   const uint32_t smem_base = smem_u32(smem_raw);
   const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
   const int part = blockIdx.x;
+  if (tid == 0) AMLA_STAMP(prm, part, 20, 0);
   if (smem_base & 1023u) {   // the swizzled tiles assume a 1024-byte aligned window
     if (tid == 0) report_timeout(prm.status);
     return;
@@ -175,9 +172,10 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
   if (plan_here && (!by_warp || wid == kLoadWarp)) plan_lengths(prm, plan_smem, lens_smem, by_warp ? lane : tid, by_warp ? 32 : kThreads);
   if (tid == 0) {
     for (int i = 0; i < C::kSlots; ++i) { mbar_init(bar(C::X_FULL + i), 1); mbar_init(bar(C::X_EMPTY + i), kWidenWarps); }
-    for (int i = 0; i < C::kBufs; ++i) { mbar_init(bar(C::X_AFULL + i), 4); mbar_init(bar(C::X_AEMPTY + i), 1); }
+    for (int i = 0; i < C::kKBufs; ++i) { mbar_init(bar(C::X_KFULL + i), 4); mbar_init(bar(C::X_KEMPTY + i), 1); }
+    for (int i = 0; i < C::kVBufs; ++i) { mbar_init(bar(C::X_VFULL + i), 4); mbar_init(bar(C::X_VEMPTY + i), 1); }
     mbar_init(bar(C::X_QREADY), kSoftmaxWarps);
-    for (int i = 0; i < 2; ++i) { mbar_init(bar(C::X_SFULL + i), 1); mbar_init(bar(C::X_SEMPTY + i), kSoftmaxWarps); }
+    for (int i = 0; i < C::kSBufs; ++i) { mbar_init(bar(C::X_SFULL + i), 1); mbar_init(bar(C::X_SEMPTY + i), kSoftmaxWarps); }
     mbar_init(bar(C::X_PREADY), kSoftmaxWarps);
     mbar_init(bar(C::X_PVDONE), 1);
     mbar_init(bar(C::X_MOVES), kSoftmaxWarps);
@@ -185,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
     mbar_init(bar(C::X_SUMS), kSoftmaxWarps);
     fence_mbar_init();
   }
-  if (wid == kMmaWarp) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
+  if (wid == kQkWarp) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
   if (plan_here) {
     if (by_warp) __syncwarp(); else __syncthreads();
     if (wid == kLoadWarp) plan_units(prm, plan_smem, lens_smem, first_smem, part, lane);
@@ -193,7 +191,12 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tbase = ld_shared_b32(tmem_slot);
+  // All 512 columns: they begin at 0.  (An address that is a constant keeps the issue of an MMA short.)
+  constexpr uint32_t tbase = 0;
+  if (ld_shared_b32(tmem_slot) != 0) {
+    if (tid == 0) report_timeout(prm.status);
+    return;
+  }
 
   const int* prefix = plan_here ? plan_smem : prm.prefix;
   const int* seqlens = plan_here ? lens_smem : prm.seqlens;
@@ -220,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
 
   if (wid < kSoftmaxWarps) {
     // ======================================================== Q, softmax, rescale, epilogue
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftmaxRegs));
     const uint32_t lane_base = static_cast<uint32_t>(wid * 32) << 16;
     const uint32_t o_addr = tbase + lane_base + C::kOCol;
     const uint32_t neg = smem_base + C::kOffNeg + wid * kN * 4, invs = smem_base + C::kOffInv + wid * kN * 4;
@@ -282,7 +285,9 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
       if (lane == 0) mbar_arrive(bar(C::X_QREADY));
     };
 
+    if (tid == 0) AMLA_STAMP(prm, part, 20, 1);
     if (tile.valid) load_q(tile.u, 0);
+    if (tid == 0) AMLA_STAMP(prm, part, 20, 2);
     if (tid == 0) merge_begin(prm, part);
     write_empty_items(prm, prefix, part, prm.P, 0, kN, tid, 32 * kSoftmaxWarps);
     while (ok && tile.valid) {
@@ -296,46 +301,43 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
       if (!ok) break;
       bool more = true;
       while (more) {
-        const uint32_t sb = gs & 1, s_addr = tbase + lane_base + C::kSCol + sb * kN;
-        ok = warp_wait(bar(C::X_SFULL + sb), (gs >> 1) & 1);
+        const uint32_t sb = gs % C::kSBufs, s_addr = tbase + lane_base + C::kSCol + sb * kN;
+        ok = warp_wait(bar(C::X_SFULL) + 8 * sb, (gs / C::kSBufs) & 1);
         if (!ok) break;
         tc_fence_after_sync();
+        if (tid == 0) AMLA_STAMP(prm, part, 7, gs);
         const bool plain = tile.np == 2 && (tile.t + 2) * kPage <= all_see;
         const int in_tile = 32 * wid + lane;
         const int key = in_tile < tile.np * kPage ? tile.t * kPage + in_tile : 0x7fffffff;
-        uint32_t pk[kN / 2];
-#pragma unroll
-        for (int h = 0; h < C::kParts; ++h) {
-          float y[C::kCols];
-          auto scores = [&](uint32_t (&s)[C::kCols]) {
-            tmem_ld_cols<C::kCols>(s_addr + 32 * h, s);
-            tmem_wait_ld();
-          };
-          auto logits = [&]() {                                        // a - n + 9, in octaves; the largest of the thread's
-            uint32_t s[C::kCols];
-            scores(s);
+        float y[kN];                                                   // a - n + 9, in octaves
+        // The second pass is for a tile that moved the reference (a unit's first always does).
+#pragma unroll 1
+        for (bool moved = false;;) {
+          bool move = tile.first;
+          if (moved || !move) {
             float top = -INFINITY;
 #pragma unroll
-            for (int r = 0; r < C::kCols; r += 4) {
-              uint32_t m[4], n[4];
-              ld_shared_v4(mult + 4 * (C::kCols * h + r), m[0], m[1], m[2], m[3]);
-              ld_shared_v4(neg + 4 * (C::kCols * h + r), n[0], n[1], n[2], n[3]);
+            for (int h = 0; h < C::kParts; ++h) {
+              uint32_t s[C::kCols];
+              tmem_ld_cols<C::kCols>(s_addr + C::kCols * h, s);
+              tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 4; ++i) y[r + i] = fmaf(__uint_as_float(s[r + i]), __uint_as_float(m[i]), __uint_as_float(n[i]));
+              for (int r = 0; r < C::kCols; r += 4) {
+                uint32_t m[4], n[4];
+                ld_shared_v4(mult + 4 * (C::kCols * h + r), m[0], m[1], m[2], m[3]);
+                ld_shared_v4(neg + 4 * (C::kCols * h + r), n[0], n[1], n[2], n[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[C::kCols * h + r + i] = fmaf(__uint_as_float(s[r + i]), __uint_as_float(m[i]), __uint_as_float(n[i]));
+              }
             }
             if (!plain) {
 #pragma unroll
-              for (int r = 0; r < C::kCols; ++r) y[r] = key < static_cast<int>(ld_shared_b32(vis + 4 * (C::kCols * h + r))) ? y[r] : -INFINITY;
+              for (int r = 0; r < kN; ++r) y[r] = key < static_cast<int>(ld_shared_b32(vis + 4 * r)) ? y[r] : -INFINITY;
             }
+            if (moved) break;
 #pragma unroll
-            for (int r = 0; r < C::kCols; r += 2) top = fmax3(top, y[r], y[r + 1]);
-            return top;
-          };
-          bool move = tile.first;
-          float top = 0.f;
-          if (!move) top = logits();
-          // Does any key of the tile exceed what P~ may reach?  The four warps decide together (a unit's first tile always moves).
-          if (!move) {
+            for (int r = 0; r < kN; r += 2) top = fmax3(top, y[r], y[r + 1]);
+            // Does any key of the tile exceed what P~ may reach?  The four warps decide together.
             const bool mine = __any_sync(0xffffffffu, top > kPLimit);
             const uint32_t at = smem_base + C::kOffMoves + (moves & 1) * 16;
             if (lane == 0) { st_shared_b32(at + 4 * wid, mine); mbar_arrive(bar(C::X_MOVES)); }
@@ -346,11 +348,15 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
             ld_shared_v4(at, f[0], f[1], f[2], f[3]);
             move = (f[0] | f[1] | f[2] | f[3]) != 0;
           }
-          if (move) {
+          if (!move) break;
+          moved = true;
+#pragma unroll
+          for (int h = 0; h < C::kParts; ++h) {
             // The largest logit of every row: over the warp, then over the four warps; lane r keeps row r.
             float mine = -INFINITY;
             uint32_t s[C::kCols];
-            scores(s);
+            tmem_ld_cols<C::kCols>(s_addr + C::kCols * h, s);
+            tmem_wait_ld();
 #pragma unroll
             for (int r = 0; r < C::kCols; ++r) {
               float a = __uint_as_float(s[r]) * ld_shared_f32(mult + 4 * (C::kCols * h + r));
@@ -397,22 +403,22 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
 #pragma unroll
               for (int r = 0; r < C::kCols; ++r) l[C::kCols * h + r] = lower_octaves(l[C::kCols * h + r], __shfl_sync(0xffffffffu, d_bits, r));
             }
-            logits();
           }
-          if (h == C::kParts - 1) {
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(C::X_SEMPTY + sb));         // the scores have been read
-          }
-#pragma unroll
-          for (int r = 0; r < C::kCols; r += 2) {
-            const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
-            l[C::kCols * h + r] += p0;
-            l[C::kCols * h + r + 1] += p1;
-            pk[(C::kCols * h + r) / 2] = pack_f16x2(p0, p1);
-          }
+          if (!ok) break;
         }
         if (!ok) break;
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::X_SEMPTY) + 8 * sb);         // the scores have been read
+        uint32_t pk[kN / 2];
+#pragma unroll
+        for (int r = 0; r < kN; r += 2) {
+          const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
+          l[r] += p0;
+          l[r + 1] += p1;
+          pk[r / 2] = pack_f16x2(p0, p1);
+        }
+        if (tid == 0) AMLA_STAMP(prm, part, 9, gs);
         if (gs > 0) {
           ok = warp_wait(bar(C::X_PVDONE), (gs - 1) & 1);              // the P~V of the tile before has read the P buffer
           if (!ok) break;
@@ -423,6 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::X_PREADY));
+        if (tid == 0) AMLA_STAMP(prm, part, 8, gs);
         ++gs;
         more = !tile.last();
         if (more) tile.next();
@@ -434,7 +441,9 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
       __syncwarp();
       // the next unit's Q: all Q K^T of this one have been waited for
       tile.next();
+      if (tid == 0) AMLA_STAMP(prm, part, 10, un);
       if (tile.valid) load_q(tile.u, un + 1);
+      if (tid == 0) AMLA_STAMP(prm, part, 11, un);
       // ---- epilogue: out = O / l, lse = n + log2 l
       int2 info;
       const int pslot = tile.units.slot_of(u, &info);                  // partial slot, or -1
@@ -512,209 +521,214 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
             stg_128(dst + static_cast<size_t>(rb + j) * kDv + 256 * p, __byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410), __byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
         }
       }
+      if (tid == 0) AMLA_STAMP(prm, part, 12, un);
       tc_fence_before_sync();      // O has been read: this warp's next PREADY arrival lets the next unit overwrite it
       ++un;
     }
     if (!ok && lane == 0) report_timeout(prm.status);
   } else if (wid < kSoftmaxWarps + kWidenWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWidenRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kWidenRegs));
     // ======================================================== widening: raw pages -> operand chunks in tensor memory
-    const int quad = wid & 3, group = (wid >> 2) - 1;
-    const uint32_t ring = tbase + (static_cast<uint32_t>(quad * 32) << 16) + C::kRing;
-    const uint32_t raw = smem_base + C::kOffRaw, infos = smem_base + C::kOffInfo;
-    uint32_t cc = 0;                                        // chunks so far: chunk cc is for group cc % 2
-    uint32_t kslot = 0, kpar = 0, vslot = 0;
-    auto next_slot = [&](uint32_t s) { return s + 1 == C::kSlots ? 0u : s + 1; };
-    // waits for chunk cc's place, and hands it over
-    auto place = [&]() {
-      const bool free = warp_wait(bar(C::X_AEMPTY) + 8 * (cc % C::kBufs), ((cc / C::kBufs) & 1) ^ 1);
-      tc_fence_after_sync();
-      return free;
+    const int quad = wid & 3;
+    const uint32_t raw = smem_base + C::kOffRaw, infos = smem_base + C::kOffInfo, lanes = tbase + (static_cast<uint32_t>(quad * 32) << 16);
+    const uint32_t group = (wid >> 2) & 1 ^ 1;               // of the two that take turns by chunk: warps 4-7 and 12-15, 8-11 and 16-19
+    uint32_t slot = 0, par = 0, tiles = 0;
+    [[maybe_unused]] int kc = 0;                            // (trace builds)
+    auto next_slot = [&](uint32_t x) { return x + 1 == C::kSlots ? 0u : x + 1; };
+    auto pages_here = [&](uint32_t slot1) {
+      ok = mbar_wait_inline(bar(C::X_FULL) + 8 * slot, par);
+      if (slot1 != slot) ok &= mbar_wait_inline(bar(C::X_FULL) + 8 * slot1, slot1 == 0 ? par ^ 1 : par);
     };
-    auto hand_over = [&]() {
+    auto pages_done = [&](uint32_t slot1) {                  // (what was read of them is in registers)
+      __syncwarp();
+      mbar_arrive_if(lane == 0, bar(C::X_EMPTY) + 8 * slot);
+      mbar_arrive_if(lane == 0 && slot1 != slot, bar(C::X_EMPTY) + 8 * slot1);
+      if (slot1 < slot) par ^= 1;
+      slot = next_slot(slot1);
+      if (slot == 0) par ^= 1;
+      ++tiles;
+      tile.next();
+    };
+    auto place = [&](uint32_t empty, uint32_t use) {
+      ok &= mbar_wait_inline(empty, (use & 1) ^ 1);
+      __syncwarp();
+      tc_fence_after_sync();
+    };
+    auto hand_over = [&](uint32_t full) {
       tmem_wait_st();
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::X_AFULL) + 8 * (cc % C::kBufs));
+      mbar_arrive_if(lane == 0, full);
     };
-    Tiles vt = tile;
-    auto widen_k = [&](int np) {                            // lane = key of the tile, 64 columns a chunk
-      const uint32_t slot1 = np == 2 ? next_slot(kslot) : kslot;
-      ok = warp_wait(bar(C::X_FULL) + 8 * kslot, kpar);
-      if (ok && np == 2) ok = warp_wait(bar(C::X_FULL) + 8 * slot1, slot1 == 0 ? kpar ^ 1 : kpar);
-      if (!ok) return;
-      const uint32_t slot = quad < 2 ? kslot : slot1, key = 32 * (quad & 1) + lane;
-      const uint32_t codes = raw + slot * kPageBytes4 + key * kCodeRow, scales = raw + slot * kPageBytes4 + kCodeBytes + key * kScaleRow;
-      const uint32_t there = ld_shared_b32(infos + 4 * slot) != 0 ? 0xffffffffu : 0u;      // a page outside the cache: zeros
+    if (wid < kSoftmaxWarps + kWidenWarps / 2) {
+      // ---- K: lane = key of the tile, 64 columns a chunk, 32 at a time
+      while (tile.valid) {
+        const uint32_t slot1 = tile.np == 2 ? next_slot(slot) : slot;
+        pages_here(slot1);
+        const uint32_t mine = quad < 2 ? slot : slot1, key = 32 * (quad & 1) + lane;
+        const uint32_t codes = raw + mine * kPageBytes4 + key * kCodeRow, scales = raw + mine * kPageBytes4 + kCodeBytes + key * kScaleRow;
+        const uint32_t there = ld_shared_b32(infos + 4 * mine) != 0 ? 0xffffffffu : 0u;      // a page outside the cache: zeros
 #pragma unroll 1
-      for (int c = 0; c < kColBlocks; ++c, ++cc) {
-        if ((cc & 1) != static_cast<uint32_t>(group)) continue;
-        uint32_t w[8], r[32];
-        ld_shared_v4(codes + 32 * c, w[0], w[1], w[2], w[3]);
-        ld_shared_v4(codes + 32 * c + 16, w[4], w[5], w[6], w[7]);
-        const uint32_t s = ld_shared_b32(scales + 4 * c) & there;
-        const uint32_t s01 = e4m3x2_to_f16x2(s & 0xffffu), s23 = e4m3x2_to_f16x2(s >> 16);
-        const uint32_t sc[4] = {__byte_perm(s01, 0, 0x1010), __byte_perm(s01, 0, 0x3232), __byte_perm(s23, 0, 0x1010), __byte_perm(s23, 0, 0x3232)};
+        for (uint32_t c = (group + tiles) & 1; c < kColBlocks; c += 2) {      // (nine a tile: the groups change places)
+          if (quad == 0 && lane == 0) AMLA_STAMP(prm, part, 0, tiles * 9 + c);
+          uint32_t w[8];
+          ld_shared_v4(codes + 32 * c, w[0], w[1], w[2], w[3]);
+          ld_shared_v4(codes + 32 * c + 16, w[4], w[5], w[6], w[7]);
+          const uint32_t sw = ld_shared_b32(scales + 4 * c) & there;
+          const uint32_t buf = c % C::kKBufs;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t x[4];
-          e2m1x8_to_f16x2(w[j], x);
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[16];
+            const uint32_t s2 = e4m3x2_to_f16x2(h == 0 ? sw & 0xffffu : sw >> 16);
+            const uint32_t sc[2] = {__byte_perm(s2, 0, 0x1010), __byte_perm(s2, 0, 0x3232)};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) r[4 * j + i] = mul_f16x2(x[i], sc[j / 2]);
-        }
-        ok = place();
-        if (!ok) return;
-        tmem_st_32x32b_x32(ring + 32 * (cc % C::kBufs), r);
-        hand_over();
-      }
-      kslot = next_slot(kslot);
-      if (kslot == 0) kpar ^= 1;
-      if (np == 2) { kslot = next_slot(kslot); if (kslot == 0) kpar ^= 1; }
-    };
-    // Lanes = V's columns, 32 keys a chunk.  A thread (g = lane / 4, q = lane % 4) takes the 32-bit words g, eight neighbouring
-    // columns, of warp `quad`'s 64 columns, for eight keys: words of two keys are interleaved by nibbles and converted, which
-    // gives pairs of keys.  Column i of a word goes to block 2p + i / 4, lane 32 quad + g + 8 (i % 4).  A step of the product is 16 keys, k = 4 q + e:
-    // key 4 q + (q + e) % 4, so that the four q read four different residues (a row is 72 words: else all from the same banks).
-    // A scale that is a NaN becomes a number here: through K the rows that see the key have a NaN for its P~, and those that do
-    // not have a zero, which a NaN in V would turn into one.
-    auto widen_v = [&](int np, int t, int n_b) {
-      const uint32_t slot1 = np == 2 ? next_slot(vslot) : vslot;
-      const int g = lane >> 2, q = lane & 3;
-#pragma unroll 1
-      for (int c = 0; c < kVChunks; ++c, ++cc) {
-        if ((cc & 1) != static_cast<uint32_t>(group)) continue;
-        const int p = c >> 2, kq = c & 3;
-        const uint32_t slot = kq < 2 ? vslot : slot1;
-        const uint32_t page = raw + slot * kPageBytes4, first = 32 * (kq & 1);
-        const int count = (kq < 2 || np == 2 ? static_cast<int>(ld_shared_b32(infos + 4 * slot)) : 0) - static_cast<int>(first);   // keys of this quarter that count
-        uint32_t r[2][2][8];
+            for (int j = 0; j < 4; ++j) {
+              uint32_t x[4];
+              e2m1x8_to_f16x2(w[4 * h + j], x);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          uint32_t w[4], s[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int in_quarter = 16 * b + 4 * q + ((q + e) & 3);
-            const uint32_t key = first + in_quarter;
-            w[e] = ld_shared_b32(page + key * kCodeRow + 32 * (4 * p + quad) + 4 * g);
-            s[e] = ld_shared_u8(page + kCodeBytes + key * kScaleRow + 4 * (4 * p + quad) + (g >> 1));
-          }
-          if (count < 32) {                                 // what is beyond the sequence's end may be anything: a scale of zero
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] = 16 * b + 4 * q + ((q + e) & 3) < count ? s[e] : 0u;
-          }
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {                     // keys e = 2j, 2j + 1
-            const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1];
-            const uint32_t even = (w0 & 0x0f0f0f0fu) | ((w1 << 4) & 0xf0f0f0f0u), odd = ((w0 >> 4) & 0x0f0f0f0fu) | (w1 & 0xf0f0f0f0u);
-            const uint32_t sc = number_f16x2(e4m3x2_to_f16x2(s[2 * j] | (s[2 * j + 1] << 8)));
-            uint32_t x[4], z[4];
-            e2m1x8_to_f16x2(even, x);
-            e2m1x8_to_f16x2(odd, z);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {                   // columns 2i (lanes .. + g) and 2i + 1 (.. + 8 + g)
-              r[i >> 1][i & 1][4 * b + j] = mul_f16x2(x[i], sc);
-              r[i >> 1][i & 1][4 * b + 2 + j] = mul_f16x2(z[i], sc);
+              for (int i = 0; i < 4; ++i) r[4 * j + i] = mul_f16x2(x[i], sc[j / 2]);
             }
+            if (h == 0) place(bar(C::X_KEMPTY) + 8 * buf, tiles + c / C::kKBufs);
+            tmem_st_32x32b_x16(lanes + C::kKCol + 32 * buf + 16 * h, r);
           }
+          hand_over(bar(C::X_KFULL) + 8 * buf);
         }
-        ok = place();
-        if (!ok) return;
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) tmem_st_16x256b_x2(ring + (static_cast<uint32_t>(16 * hh) << 16) + 32 * (cc % C::kBufs) + 16 * m, r[m][hh]);
-        hand_over();
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        pages_done(slot1);
       }
-      if (lane == 0) {                                      // (the words are in registers, and in tensor memory)
-        mbar_arrive(bar(C::X_EMPTY) + 8 * vslot);
-        if (np == 2) mbar_arrive(bar(C::X_EMPTY) + 8 * slot1);
+    } else {
+      // ---- V: lanes = its columns, 32 keys a chunk, 16 at a time.  A thread (g = lane / 4, q = lane % 4) takes the 32-bit words g, eight
+      // neighbouring columns, of warp `quad`'s 64 columns, for four keys: words of two keys are interleaved by nibbles and converted, which
+      // gives pairs of keys.  Column i of a word goes to block 2p + i / 4, lane 32 quad + g + 8 (i % 4).  Key k = 4 q + e of the product's 16 is
+      // key 4 q + (q + e) % 4, so that the four q read four different residues (a row is 72 words: else all from the same banks).
+      // A scale that is a NaN becomes a number here: through K the rows that see the key have a NaN for its P~, and those that do
+      // not have a zero, which a NaN in V would turn into one.
+      const int g = lane >> 2, q = lane & 3;
+      const uint32_t pick = (g >> 1) | ((4 + (g >> 1)) << 4);   // this thread's group, of the four that a scale word holds, of either key
+      while (tile.valid) {
+        const uint32_t slot1 = tile.np == 2 ? next_slot(slot) : slot;
+        pages_here(slot1);
+#pragma unroll 1
+        for (uint32_t c = group; c < kVChunks; c += 2) {
+          if (quad == 0 && lane == 0) AMLA_STAMP(prm, part, 13, tiles * 8 + c);
+          const uint32_t mine = (c & 2) ? slot1 : slot, buf = c & (C::kVBufs - 1);
+          const uint32_t page = raw + mine * kPageBytes4, codes = page + (c & 1) * (32 * kCodeRow) + (c >> 2) * 128 + 32 * quad + 4 * g;
+          const uint32_t scales = page + kCodeBytes + (c & 1) * (32 * kScaleRow) + (c >> 2) * 16 + 4 * quad;
+          const int count = ((c & 2) && tile.np == 1 ? 0 : static_cast<int>(ld_shared_b32(infos + 4 * mine))) - 32 * static_cast<int>(c & 1);   // keys of the chunk that count
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint32_t w[4], sw[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t key = 4 * q + ((q + e) & 3);
+              w[e] = ld_shared_b32(codes + key * kCodeRow + 16 * b * kCodeRow);
+              sw[e] = ld_shared_b32(scales + key * kScaleRow + 16 * b * kScaleRow);
+            }
+            if (count < 32) {                                 // what is beyond the sequence's end may be anything: scales of zero
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sw[e] = 16 * b + 4 * q + ((q + e) & 3) < count ? sw[e] : 0u;
+            }
+            uint32_t r[2][2][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {                     // keys e = 2j, 2j + 1
+              const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1];
+              const uint32_t even = (w0 & 0x0f0f0f0fu) | ((w1 << 4) & 0xf0f0f0f0u), odd = ((w0 >> 4) & 0x0f0f0f0fu) | (w1 & 0xf0f0f0f0u);
+              const uint32_t sc = number_f16x2(e4m3x2_to_f16x2(__byte_perm(sw[2 * j], sw[2 * j + 1], pick)));
+              uint32_t x[4], z[4];
+              e2m1x8_to_f16x2(even, x);
+              e2m1x8_to_f16x2(odd, z);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {                   // columns 2i (lanes .. + g) and 2i + 1 (.. + 8 + g)
+                r[i >> 1][i & 1][j] = mul_f16x2(x[i], sc);
+                r[i >> 1][i & 1][2 + j] = mul_f16x2(z[i], sc);
+              }
+            }
+            if (b == 0) place(bar(C::X_VEMPTY) + 8 * buf, C::kVBufs == 4 ? c >> 2 : c >> 1);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh) tmem_st_16x256b_x1(lanes + (static_cast<uint32_t>(16 * hh) << 16) + C::kVCol + 32 * buf + 16 * m + 8 * b, r[m][hh]);
+          }
+          hand_over(bar(C::X_VFULL) + 8 * buf);
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        pages_done(slot1);
       }
-      vslot = next_slot(slot1);
-    };
-    // The order of the MMA warp.  K is always one tile ahead of V, but at the end of a unit (tile is the one behind vt, or vt's own while
-    // a unit begins).
-    auto k_next = [&]() { widen_k(tile.np); tile.next(); };
-    if (tile.valid) k_next();
-    while (ok && vt.valid) {
-      if (tile.valid && !tile.first) k_next();
-      if (!ok) break;
-      widen_v(vt.np, vt.t, vt.u.n_b);
-      if (!ok) break;
-      vt.next();
-      if (vt.valid && vt.first) k_next();
     }
     if (!ok && lane == 0) report_timeout(prm.status);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
-    if (wid == kMmaWarp) {
-    // ======================================================== MMAs
-    if (elect_one()) {
-      constexpr uint32_t idesc_s = make_idesc_f16(128, kN, false, false), idesc_o = make_idesc_f16(128, kN, false, true);
-      constexpr uint32_t dhi = smem_desc_hi_sw128(1024);
-      const uint32_t qlo = smem_desc_lo(smem_base, 16), plo = smem_desc_lo(smem_base + C::kOffP, 16);
-      const uint32_t ring = tbase + C::kRing;
-      uint32_t cc = 0, gs = 0, gp = 0, un = 0;
-      Tiles vt = tile;
-      auto chunk = [&]() {
-        ok = mbar_wait(bar(C::X_AFULL) + 8 * (cc % C::kBufs), (cc / C::kBufs) & 1);
-        if (ok) tc_fence_after_sync();
-        return ok;
-      };
-      auto qk = [&]() {
-        if (tile.first) {
-          ok = mbar_wait(bar(C::X_QREADY), un & 1);
-          if (!ok) return;
-          ++un;
-        }
-        const uint32_t sb = gs & 1, d = tbase + C::kSCol + sb * kN;
-        ok = mbar_wait(bar(C::X_SEMPTY) + 8 * sb, ((gs >> 1) & 1) ^ 1);
-        if (!ok) return;
-        tc_fence_after_sync();
-        uint32_t ql = qlo;
-#pragma unroll 1
-        for (int c = 0; c < kColBlocks; ++c) {
-          if (!chunk()) return;
-          const uint32_t a = ring + 32 * (cc % C::kBufs);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
+    constexpr uint32_t dhi = smem_desc_hi_sw128(1024);
+    if (wid == kQkWarp) {
+      // ======================================================== S^T = K Q^T
+      // (Constants wherever they can be: an accumulate flag out of a register alone costs as much issue as an MMA.)
+      if (elect_one()) {
+        constexpr uint32_t idesc = make_idesc_f16(128, kN, false, false);
+        uint32_t gs = 0, un = 0, par = 0;
+        while (tile.valid) {
+          if (tile.first) ok = mbar_wait_inline(bar(C::X_QREADY), un++ & 1);
+          const uint32_t sb = gs % C::kSBufs, d = C::kSCol + sb * kN;
+          ok &= mbar_wait_inline(bar(C::X_SEMPTY) + 8 * sb, ((gs / C::kSBufs) & 1) ^ 1);
+          tc_fence_after_sync();
+          constexpr uint32_t kQStep = C::kQBlock >> 4;
+          const uint32_t ql = smem_desc_lo(smem_base, 16);
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) mma_ts(d, a + 8 * kk, smem_desc_join(ql + 2 * kk, dhi), idesc_s, (c | kk) != 0);
-          mma_commit(bar(C::X_AEMPTY) + 8 * (cc % C::kBufs));
-          ++cc;
-          ql += C::kQBlock >> 4;
-        }
-        mma_commit(bar(C::X_SFULL) + 8 * sb);
-        ++gs;
-        tile.next();
-      };
-      auto pv = [&]() {
-        ok = mbar_wait(bar(C::X_PREADY), gp & 1);
-        if (!ok) return;
-        tc_fence_after_sync();
-        const uint32_t acc = vt.first ? 0u : 1u;
-#pragma unroll 1
-        for (int c = 0; c < kVChunks; ++c) {
-          if (!chunk()) return;
-          const uint32_t a = ring + 32 * (cc % C::kBufs), kq = c & 3;
-          const uint32_t d = tbase + C::kOCol + 2 * kN * (c >> 2), pl = plo + kq * (32 * 128 >> 4);
+          for (int c = 0; c < kColBlocks; ++c) {
+            constexpr int kB = C::kKBufs;
+            ok &= mbar_wait_inline(bar(C::X_KFULL + c % kB), par ^ ((c / kB) & 1));
+            tc_fence_after_sync();
+            AMLA_STAMP(prm, part, 5, gs * 9 + c);
 #pragma unroll
-          for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) mma_ts(d + kN * m, a + 16 * m + 8 * kk, smem_desc_join(pl + kk * (16 * 128 >> 4), dhi), idesc_o, (kq | kk) != 0 ? 1u : acc);
-          mma_commit(bar(C::X_AEMPTY) + 8 * (cc % C::kBufs));
-          ++cc;
+            for (int kk = 0; kk < 4; ++kk)
+              mma_ts(d, C::kKCol + 32 * (c % kB) + 8 * kk, smem_desc_join(ql + c * kQStep + 2 * kk, dhi), idesc, c == 0 && kk == 0 ? 0 : 1);
+            mma_commit(bar(C::X_KEMPTY + c % kB));
+          }
+          mma_commit(bar(C::X_SFULL) + 8 * sb);
+          if (!ok) break;
+          par ^= 1;                                          // (nine chunks in three places)
+          ++gs;
+          tile.next();
         }
-        mma_commit(bar(C::X_PVDONE));
-        ++gp;
-        vt.next();
-      };
-      if (tile.valid) qk();
-      while (ok && vt.valid) {
-        if (tile.valid && !tile.first) qk();
-        if (ok) pv();
-        if (ok && vt.valid && vt.first) qk();
+        if (!ok) report_timeout(prm.status);
       }
-      if (!ok) report_timeout(prm.status);
-    }
-    __syncwarp();
+      __syncwarp();
+    } else if (wid == kPvWarp) {
+      // ======================================================== O^T (+)= V^T P~^T
+      if (elect_one()) {
+        constexpr uint32_t idesc = make_idesc_f16(128, kN, false, true);
+        uint32_t gp = 0;
+        while (tile.valid) {
+          ok = mbar_wait_inline(bar(C::X_PREADY), gp & 1);
+          tc_fence_after_sync();                              // (O may have been rescaled)
+          const uint32_t pl = smem_desc_lo(smem_base + C::kOffP, 16);
+          const bool fresh = tile.first;
+#pragma unroll
+          for (int c = 0; c < kVChunks; ++c) {
+            constexpr int kB = C::kVBufs;
+            const int p = c >> 2, kq = c & 3;
+            ok &= mbar_wait_inline(bar(C::X_VFULL + c % kB), (c / kB) & 1);
+            tc_fence_after_sync();
+            AMLA_STAMP(prm, part, 17, gp * 8 + c);
+            const uint32_t a = C::kVCol + 32 * (c % kB), pc = pl + kq * (32 * 128 >> 4);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              const uint32_t d = C::kOCol + kN * (2 * p + m);
+              if (kq == 0 && fresh) mma_ts(d, a + 16 * m, smem_desc_join(pc, dhi), idesc, 0);
+              else mma_ts(d, a + 16 * m, smem_desc_join(pc, dhi), idesc, 1);
+              mma_ts(d, a + 16 * m + 8, smem_desc_join(pc + (16 * 128 >> 4), dhi), idesc, 1);
+            }
+            mma_commit(bar(C::X_VEMPTY + c % kB));
+          }
+          mma_commit(bar(C::X_PVDONE));
+          if (!ok) break;
+          ++gp;
+          tile.next();
+        }
+        if (!ok) report_timeout(prm.status);
+      }
+      __syncwarp();
     } else if (wid == kLoadWarp) {
     // ======================================================== pages in order
     if (elect_one()) {
@@ -726,7 +740,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
         const int here = page, keys = min(kPage, tile.u.n_b - (tile.t + i) * kPage);
         if (++i == tile.np) { i = 0; tile.next(); }
         if (tile.valid) page = entry();                     // on its way while this page waits for its slot
-        ok = mbar_wait(bar(C::X_EMPTY) + 8 * slot, par);
+        ok = mbar_wait_inline(bar(C::X_EMPTY) + 8 * slot, par);
         if (!ok) break;
         const bool there = here >= 0 && here < prm.num_blocks;
         const uint32_t full = bar(C::X_FULL) + 8 * slot;
@@ -745,7 +759,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
         // let the copies that may still be in flight land before the CTA exits
         for (uint32_t k = 0; k < C::kSlots && k < n_issued; ++k) {
           const uint32_t j = n_issued - 1 - k;
-          mbar_wait(bar(C::X_FULL) + 8 * (j % C::kSlots), (j / C::kSlots) & 1);
+          mbar_wait_inline(bar(C::X_FULL) + 8 * (j % C::kSlots), (j / C::kSlots) & 1);
         }
       }
     }
@@ -755,7 +769,8 @@ __global__ void __launch_bounds__(kThreads, 1) decode_fp4_kernel(const DecodePar
 
   tc_fence_before_sync();
   __syncthreads();
-  if (wid == kMmaWarp) tmem_dealloc(tbase, 512);
+  if (tid == 0) AMLA_STAMP(prm, part, 21, 0);
+  if (wid == kQkWarp) tmem_dealloc(tbase, 512);
 }
 
 // ---------------------------------------------------------------------------------------------------

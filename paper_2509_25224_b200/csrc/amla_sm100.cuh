@@ -8,12 +8,6 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-// What is executed seldom is kept out of line, but in a kernel that moves registers between its warpgroups (setmaxnreg), where the
-// compiler cannot place calls: such a source file defines this as __forceinline__ ahead of its includes.
-#ifndef AMLA_SELDOM
-#define AMLA_SELDOM __noinline__
-#endif
-
 namespace amla {
 namespace sm100 {
 
@@ -104,7 +98,7 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;   // 2 s: far beyond any legiti
 // Slow path of a wait, kept out of line so that the many call sites stay small (the role loops are
 // executed by single warps and are sensitive to instruction-cache footprint).
 template <bool kClusterAcquire>
-__device__ AMLA_SELDOM bool mbar_wait_slow(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
   const uint64_t t0 = global_timer_ns();
   while (true) {
     for (int i = 0; i < 256; ++i) {
@@ -119,6 +113,29 @@ template <bool kClusterAcquire = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_t limit_ns = kWaitLimitNs) {
   if (kClusterAcquire ? mbar_test_cluster_acquire(bar, parity) : mbar_test(bar, parity)) return true;
   return mbar_wait_slow<kClusterAcquire>(bar, parity, limit_ns);
+}
+
+// The same as one piece of code that runs straight through when the phase is complete, for kernels that cannot have calls in them
+// (setmaxnreg) and for loops where a taken branch (some 30 clk) counts.  It gives up after kWaitTries tries, of 20 clk at least and
+// of as long as the hardware suspends a thread otherwise: 45 ms or more.
+constexpr uint32_t kWaitTries = 1u << 22, kWaitHintNs = 1000;
+__device__ __forceinline__ bool mbar_wait_inline(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
+      "mov.u32 n, %3;\n"
+      "L_TRY_%=:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %4;\n\t"
+      "sub.u32 n, n, 1;\n\t"
+      "setp.ne.and.u32 q, n, 0, !p;\n\t"
+      "@q bra L_TRY_%=;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity), "n"(kWaitTries), "n"(kWaitHintNs) : "memory");
+  return ok != 0;
+}
+// Arrives where `yes` (no branch around it, so that a warp stays together).
+__device__ __forceinline__ void mbar_arrive_if(bool yes, uint32_t bar) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(static_cast<uint32_t>(yes)) : "memory");
 }
 
 // ------------------------------------------------------------------ fences

@@ -6,6 +6,12 @@
 #include "amla_common.cuh"
 #include "amla_sm100.cuh"
 
+// What is executed seldom is kept out of line, but in a kernel that moves registers between its warpgroups (setmaxnreg), where the
+// compiler cannot place calls: such a source file defines this as __forceinline__ ahead of its includes.
+#ifndef AMLA_SELDOM
+#define AMLA_SELDOM __noinline__
+#endif
+
 namespace amla {
 
 __device__ __forceinline__ int warp_inclusive_scan(int v, int lane) {
