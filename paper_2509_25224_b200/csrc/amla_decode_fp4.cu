@@ -41,14 +41,15 @@ constexpr int kWidenWarps = 16;                         // K: two groups of four
 constexpr int kColBlocks = kDqk / 64;                   // K chunks of a tile
 constexpr int kVChunks = 8;                             // V chunks of a tile: 16 keys, all 512 columns
 constexpr uint32_t kPBytes = 128 * 128;                 // P~: [128 keys][64 rows of f16], 128-byte swizzle
+constexpr uint32_t kTileBytes = 2 * kPageBytes4;
 constexpr int kSmemPlanItems = 512;
 constexpr float kPBias = 9.f, kPLimit = 15.f;           // P~ = 2^(a - n + 9), at most 2^15
 constexpr int kUnitsAhead = 4;                          // units that may be between Q's loading and the softmax, and one
 
-// What the loader says of a page: how many of its keys count (none: the page is outside the cache, and zeros); of a tile's first page
-// also what the widening warps have to know of the tile.
-constexpr int kUnitNotes = 16;                          // tiles (and units) between the loader and the products of V at most, and more
-constexpr uint32_t kKeysMask = 127, kTwoPages = 1 << 8, kFirstTile = 1 << 9, kNoMoreTiles = 1 << 10;
+// What the loader says of a tile: how many keys of its two pages count (none: no such page, or one outside the cache, which is zeros),
+// whether it has two, whether it opens or ends a unit, and whether it is the part's last.
+constexpr int kNotes = 16;                              // tiles (and units) between the loader and the products of V at most, and more
+constexpr uint32_t kKeysMask = 127, kSecondPage = 8, kTwoPages = 1 << 15, kFirstTile = 1 << 16, kEndsUnit = 1 << 17, kLastTile = 1 << 18;
 
 template <int kN>
 struct Shape {
@@ -61,14 +62,14 @@ struct Shape {
   static constexpr int kLaunchRegs = 65536 / kThreads / 8 * 8;
   static constexpr int kSoftmaxRegs = kN == 64 ? 112 : 136, kWidenRegs = kN == 64 ? 56 : 72, kIssueRegs = 56;
   static_assert(kGroups * kSoftmaxRegs + 4 * kWidenRegs + kIssueRegs <= kThreads / 128 * kLaunchRegs, "the block has no more to give out");
-  static constexpr int kSlots = kN == 64 ? 6 : kN == 32 ? 8 : 9;      // pages in shared memory
+  static constexpr int kSlots = kN == 64 ? 3 : 4;       // tiles (two pages) in shared memory
   // Operand chunks in tensor memory, of K and of V: numbers that divide a tile's, so that a tile's chunks always have the same places.
   static constexpr int kKBufs = 3, kVBufs = kN == 64 ? 2 : 4;
   static constexpr int kSBufs = kN == 64 ? 1 : 2;       // score tiles in tensor memory
   static constexpr uint32_t kQBlock = kN * 128;         // [rows][64 columns of f16], 128-byte swizzle
   static constexpr uint32_t kOffP = kColBlocks * kQBlock;
   static constexpr uint32_t kOffRaw = kOffP + kPBytes;
-  static constexpr uint32_t kOffMult = kOffRaw + kSlots * kPageBytes4;      // float [units ahead][rows]: logit per product, in octaves
+  static constexpr uint32_t kOffMult = kOffRaw + kSlots * kTileBytes;      // float [units ahead][rows]: logit per product, in octaves
   static constexpr uint32_t kOffVis = kOffMult + kUnitsAhead * kN * 4;      // int [units ahead][rows]: keys that the row sees
   static constexpr uint32_t kOffNeg = kOffVis + kUnitsAhead * kN * 4;       // float [softmax warps][columns]: 9 - n
   static constexpr uint32_t kOffAdd = kOffNeg + kSoftmaxWarps * kCols * 4;  // float [softmax warps][columns]: the octaves of a move; 1 / l at the end
@@ -76,10 +77,10 @@ struct Shape {
   static constexpr uint32_t kOffMax = kOffSums + 2 * kSoftmaxWarps * kCols * 4;   // float [2][softmax warps][32]
   static constexpr uint32_t kOffMoves = kOffMax + 2 * kSoftmaxWarps * 32 * 4;     // uint32 [2][softmax warps]
   static_assert(kOffMoves % 16 == 0 && kOffNeg % 16 == 0, "read four at a time");
-  static constexpr uint32_t kOffInfo = kOffMoves + 2 * kSoftmaxWarps * 4;                      // int [slots]: keys of the page that count
-  static constexpr uint32_t kOffUnits = kOffInfo + 48;                      // int4 [unit notes]: sequence, first row, keys
-  static constexpr uint32_t kOffTiles = kOffUnits + kUnitNotes * 16;        // uint32 [tile notes]: kFirstTile, kNoMoreTiles (behind it)
-  static constexpr uint32_t kOffBars = kOffTiles + kUnitNotes * 4;
+  static constexpr uint32_t kOffNotes = kOffMoves + 2 * kSoftmaxWarps * 4;  // uint2 [notes]: what the loader says of a tile, its first key
+  static constexpr uint32_t kOffUnits = kOffNotes + kNotes * 8;             // int4 [notes][2] of a unit: sequence, first row, keys, -; slot of its partial (-1:
+                                                                            // none), item, slot of the item's first partial, partials
+  static constexpr uint32_t kOffBars = kOffUnits + kNotes * 32;
   static constexpr uint32_t kBarBytes = 384;
   static constexpr uint32_t kOffPlan = kOffBars + kBarBytes;
   static constexpr uint32_t kOffLens = kOffPlan + ((kSmemPlanItems + 1) * 4 + 15) / 16 * 16;
@@ -92,8 +93,8 @@ struct Shape {
          X_START = X_SUMS + kGroups, X_NUM };
   static_assert(X_NUM * 8 + 8 <= kBarBytes, "barrier area too small");
   static_assert(kBytes <= 232448, "exceeds the shared memory a block can opt in to");
-  static_assert(kOffP % 1024 == 0 && kOffRaw % 1024 == 0 && kPageBytes4 % 16 == 0 && kOffBars % 8 == 0, "alignment");
-  static_assert(kSCol + kSBufs * kN <= kKCol && kSlots <= 12 && kSlots < kUnitNotes, "tensor memory");
+  static_assert(kOffP % 1024 == 0 && kOffRaw % 1024 == 0 && kTileBytes % 16 == 0 && kOffBars % 8 == 0, "alignment");
+  static_assert(kSCol + kSBufs * kN <= kKCol && kSlots + 4 < kNotes, "tensor memory");
   static_assert(kColBlocks % kKBufs == 0 && kVChunks % kVBufs == 0 && (kVBufs == 2 || kVBufs == 4), "places of chunks");
 };
 
@@ -203,9 +204,11 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
     if (by_warp) __syncwarp(); else __syncthreads();
     if (wid == kLoadWarp) plan_units(prm, plan_smem, lens_smem, first_smem, part, lane);
   }
+  if (tid == 0) AMLA_STAMP(prm, part, 20, 1);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
+  if (tid == 0) AMLA_STAMP(prm, part, 20, 2);
   // All 512 columns: they begin at 0.  (An address that is a constant keeps the issue of an MMA short.)
   constexpr uint32_t tbase = 0;
   if (ld_shared_b32(tmem_slot) != 0) {
@@ -217,6 +220,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
   const int* seqlens = plan_here ? lens_smem : prm.seqlens;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
+  if (tid == 0) AMLA_STAMP(prm, part, 20, 3);
   if (plan_here) {
     if (plan_is_stale(prm, plan_smem, lens_smem, first_smem, tid, kThreads)) {
       plan_lengths(prm, plan_smem, lens_smem, tid, kThreads);
@@ -233,13 +237,13 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
     }
     __syncthreads();
   }
+  if (tid == 0) AMLA_STAMP(prm, part, 20, 4);
   bool ok = true;
   const FirstUnit* first = plan_here ? first_smem : nullptr;
 
   if (wid < kSoftmaxWarps) {
     // ======================================================== softmax, rescale, epilogue
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftmaxRegs));
-    Tiles tile(UnitIter(prm, prefix, seqlens, part), first);
     constexpr int kCols = C::kCols;
     const int quad = wid & 3, group = wid >> 2, col0 = group * kCols;  // this group's rows are col0 ..
     const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
@@ -251,9 +255,10 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
     uint32_t gs = 0, un = 0, moves = 0, maxes = 0;
     if (tid == 0) merge_begin(prm, part);
     write_empty_items(prm, prefix, part, prm.P, 0, kN, tid, 32 * kSoftmaxWarps);
-    while (ok && tile.valid) {
-      const Unit u = tile.u;
-      const int all_see = max(u.n_b - prm.Sq + 1, 0);                  // keys in front of this one are seen by every row
+    ok = warp_wait(bar(C::X_START), 0);
+    bool units_left = ok && static_cast<int>(ld_shared_b32(smem_base + C::kOffUnits + 8)) > 0;
+    while (units_left) {
+      const uint32_t unit = smem_base + C::kOffUnits + (un % kNotes) * 32;
       const uint32_t mult = smem_base + C::kOffMult + ((un % kUnitsAhead) * kN + col0) * 4, vis = smem_base + C::kOffVis + ((un % kUnitsAhead) * kN + col0) * 4;
       float l[kCols];
 #pragma unroll
@@ -262,8 +267,8 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       __syncwarp();
       ok = warp_wait(bar(C::X_QREADY + un % kUnitsAhead), (un / kUnitsAhead) & 1);   // mult, vis
       if (!ok) break;
-      bool more = true;
-      while (more) {
+      uint32_t note = 0;
+      do {
         const uint32_t sb = gs % C::kSBufs;
         ok = warp_wait(bar(C::X_SFULL) + 8 * sb, (gs / C::kSBufs) & 1);
         if (!ok) break;
@@ -286,14 +291,18 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
             for (int i = 0; i < 4; ++i) y[r + i] = fmaf(__uint_as_float(s[r + i]), __uint_as_float(m[i]), __uint_as_float(n[i]));
           }
         }
-        const bool plain = tile.np == 2 && (tile.t + 2) * kPage <= all_see;
+        uint32_t key0;
+        ld_shared_v2(smem_base + C::kOffNotes + 8 * (gs % kNotes), note, key0);
+        const bool first = note & kFirstTile, two = note & kTwoPages;
+        // all rows see what is in front of their sequence's last Sq - 1 keys
+        const bool plain = two && static_cast<int>(key0) + 2 * kPage <= static_cast<int>(ld_shared_b32(unit + 8)) - prm.Sq + 1;
         if (!plain) {
           const int in_tile = 32 * quad + lane;
-          const int key = in_tile < tile.np * kPage ? tile.t * kPage + in_tile : 0x7fffffff;
+          const int key = two || in_tile < kPage ? static_cast<int>(key0) + in_tile : 0x7fffffff;
 #pragma unroll
           for (int r = 0; r < kCols; ++r) y[r] = key < static_cast<int>(ld_shared_b32(vis + 4 * r)) ? y[r] : -INFINITY;
         }
-        bool move = tile.first;
+        bool move = first;
         if (!move) {
           // Does any key of the tile exceed what P~ may reach?  The group's four warps decide together.
           float top = -INFINITY;
@@ -330,7 +339,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           // Every row whose maximum rose above the reference moves to it (moving early is always allowed), in a unit's first tile all do.
           float d = 0.f;
           if (lane < kCols) {
-            if (tile.first ? mine > -INFINITY : mine > kPBias) d = kPBias - ceilf(mine);
+            if (first ? mine > -INFINITY : mine > kPBias) d = kPBias - ceilf(mine);
             st_shared_b32(neg + 4 * lane, __float_as_uint(ld_shared_f32(neg + 4 * lane) + d));
             st_shared_b32(add + 4 * lane, __float_as_uint(d));
           }
@@ -342,7 +351,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[r + i] += __uint_as_float(x[i]);
           }
-          if (!tile.first) {
+          if (!first) {
             // O <- AS_FP32(AS_INT32(O) + d * 2^23): O^T has a row per column, a thread the same d for all of a row
             const int d_bits = static_cast<int>(fmaxf(d, -255.f)) * (1 << 23);
             ok = warp_wait(bar(C::X_PVDONE), (gs - 1) & 1);
@@ -383,16 +392,15 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
         mbar_arrive_if(lane == 0, bar(C::X_PREADY));
         if (tid == 0) AMLA_STAMP(prm, part, 8, gs);
         ++gs;
-        more = !tile.last();
-        if (more) tile.next();
-      }
+      } while (!(note & kEndsUnit));
       if (!ok) break;
       // ---- epilogue: out = O / l, lse = n + log2 l
-      tile.next();
       if (tid == 0) AMLA_STAMP(prm, part, 10, un);
-      int2 info;
-      const int pslot = tile.units.slot_of(u, &info);                  // partial slot, or -1
-      if (tid == 0) merge_note(prm, part, u.it, info);
+      uint32_t u_b, u_r0, u_n, unused, u_slot, u_item, info_x, info_y;
+      ld_shared_v4(unit, u_b, u_r0, u_n, unused);
+      ld_shared_v4(unit + 16, u_slot, u_item, info_x, info_y);
+      const int pslot = static_cast<int>(u_slot);                      // partial slot, or -1
+      if (tid == 0) merge_note(prm, part, u_item, make_int2(info_x, info_y));
       const uint32_t sums = smem_base + C::kOffSums + ((un & 1) * kSoftmaxWarps + 4 * group) * (kCols * 4) + 4 * (lane % kCols);
       const float mine = sum_rows<kCols>(l, lane);
       if (lane < kCols) st_shared_b32(sums + quad * (kCols * 4), __float_as_uint(mine));
@@ -400,8 +408,8 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       mbar_arrive_if(lane == 0, bar(C::X_SUMS + group));
       ok = warp_wait(bar(C::X_SUMS + group), un & 1);
       if (!ok) break;
-      const size_t row0 = static_cast<size_t>(u.b) * prm.R + u.r0 + col0, prow0 = static_cast<size_t>(pslot < 0 ? 0 : pslot) * kN + col0;
-      const int rows = prm.R - u.r0 - col0;                            // live ones among the group's
+      const size_t row0 = static_cast<size_t>(u_b) * prm.R + u_r0 + col0, prow0 = static_cast<size_t>(pslot < 0 ? 0 : pslot) * kN + col0;
+      const int rows = prm.R - static_cast<int>(u_r0) - col0;                            // live ones among the group's
       // A partial is an average of values of at most 2688, in half precision as it is; the power of two of out_scale is its chunks' scale
       // byte, the rest of out_scale (in [1, 2)) is multiplied in.
       const uint32_t scale_bits = __float_as_uint(prm.out_scale);
@@ -459,38 +467,28 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       if (tid == 0) AMLA_STAMP(prm, part, 12, un);
       tc_fence_before_sync();      // O has been read: this warp's next PREADY arrival lets the next unit overwrite it
       ++un;
+      units_left = !(note & kLastTile);
     }
     if (!ok && lane == 0) report_timeout(prm.status);
   } else if (wid < kSoftmaxWarps + kWidenWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kWidenRegs));
     // ======================================================== widening: raw pages -> operand chunks in tensor memory
     const int quad = wid & 3;
-    const uint32_t raw = smem_base + C::kOffRaw, infos = smem_base + C::kOffInfo, lanes = tbase + (static_cast<uint32_t>(quad * 32) << 16);
+    const uint32_t raw = smem_base + C::kOffRaw, lanes = tbase + (static_cast<uint32_t>(quad * 32) << 16);
     const uint32_t group = ((wid - C::kKWarp) >> 2) & 1;     // of the two that take turns by chunk
-    uint32_t slot = 0, slot1 = 0, par = 0, tiles = 0, said = 0, said1 = 0;
-    auto next_slot = [&](uint32_t x) { return x + 1 == C::kSlots ? 0u : x + 1; };
-    // The next tile's pages: in `slot` and, if there is a second one, slot1 (else the same).  False: a wait ran out.
-    auto pages_here = [&]() {
-      ok = mbar_wait_inline(bar(C::X_FULL) + 8 * slot, par);
-      said = said1 = ld_shared_b32(infos + 4 * slot);
-      slot1 = slot;
-      if (said & kTwoPages) {
-        slot1 = next_slot(slot);
-        ok &= mbar_wait_inline(bar(C::X_FULL) + 8 * slot1, slot1 == 0 ? par ^ 1 : par);
-        said1 = ld_shared_b32(infos + 4 * slot1);
-      }
+    uint32_t slot = 0, par = 0, tiles = 0, note = 0;
+    auto tile_here = [&]() {                                 // false: the wait ran out
+      ok &= mbar_wait_inline(bar(C::X_FULL) + 8 * slot, par);
+      note = ld_shared_b32(smem_base + C::kOffNotes + 8 * (tiles % kNotes));
       ok = __all_sync(0xffffffffu, ok);
       return ok;
     };
-    auto pages_done = [&]() {                                // (what was read of them is in registers)
+    auto tile_done = [&]() {                                 // (what was read of it is in registers)
       __syncwarp();
       mbar_arrive_if(lane == 0, bar(C::X_EMPTY) + 8 * slot);
-      mbar_arrive_if(lane == 0 && slot1 != slot, bar(C::X_EMPTY) + 8 * slot1);
-      if (slot1 < slot) par ^= 1;
-      slot = next_slot(slot1);
-      if (slot == 0) par ^= 1;
+      if (++slot == C::kSlots) { slot = 0; par ^= 1; }
       ++tiles;
-      return ok && !(said1 & kNoMoreTiles);                  // (said of a tile's last page)
+      return ok && !(note & kLastTile);
     };
     auto place = [&](uint32_t empty, uint32_t use) {
       ok &= mbar_wait_inline(empty, (use & 1) ^ 1);
@@ -507,7 +505,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
     // logit and the keys that a row sees.  The bytes land where the operand is to be and are converted in place.
     auto load_q = [&](uint32_t un, int each, bool alone) {
       uint32_t b, unit_r0, n_b, unused;
-      ld_shared_v4(smem_base + C::kOffUnits + (un % kUnitNotes) * 16, b, unit_r0, n_b, unused);
+      ld_shared_v4(smem_base + C::kOffUnits + (un % kNotes) * 32, b, unit_r0, n_b, unused);
       const int left = prm.R - static_cast<int>(unit_r0);      // rows of the sequence from here on
       const __nv_bfloat16* rows = prm.q + (static_cast<size_t>(b) * prm.R + unit_r0) * kDqk;
       const uint32_t mult = smem_base + C::kOffMult + (un % kUnitsAhead) * kN * 4, vis = smem_base + C::kOffVis + (un % kUnitsAhead) * kN * 4;
@@ -558,23 +556,27 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       return ok && static_cast<int>(ld_shared_b32(smem_base + C::kOffUnits + 8)) > 0;
     };
     const bool any = any_unit();
+    if (tid == 32 * C::kKWarp) AMLA_STAMP(prm, part, 20, 5);
     if (any) load_q(0, kN / kWidenWarps, false);
+    if (tid == 32 * C::kKWarp) AMLA_STAMP(prm, part, 20, 6);
     if (!any) {
     } else if (wid < C::kVWarp) {
       uint32_t un = 1;
+      const uint32_t key = 32 * (quad & 1) + lane, page = raw + (quad >> 1) * kPageBytes4;
+      const uint32_t code_of = page + key * kCodeRow + 32 * group, scale_of = page + kCodeBytes + key * kScaleRow + 4 * group;
       // ---- K: lane = key of the tile, 64 columns a chunk
       do {
-        if (!pages_here()) break;
-        if ((said & kFirstTile) && tiles > 0) {
+        if (!tile_here()) break;
+        if (quad == 0 && lane == 0) AMLA_STAMP(prm, part, 19, tiles);
+        if ((note & kFirstTile) && tiles > 0) {
           // the products of the unit before have read its Q
           ok = warp_wait(bar(C::X_SFULL) + 8 * ((tiles - 1) % C::kSBufs), ((tiles - 1) / C::kSBufs) & 1);
           if (!ok) break;
           load_q(un, kN / (kWidenWarps / 2), true);
           ++un;
         }
-        const uint32_t mine = quad < 2 ? slot : slot1, key = 32 * (quad & 1) + lane;
-        uint32_t codes = raw + mine * kPageBytes4 + key * kCodeRow + 32 * group, scales = raw + mine * kPageBytes4 + kCodeBytes + key * kScaleRow + 4 * group;
-        const uint32_t there = ((quad < 2 ? said : said1) & kKeysMask) != 0 ? 0xffffffffu : 0u;
+        uint32_t codes = code_of + slot * kTileBytes, scales = scale_of + slot * kTileBytes;
+        const uint32_t there = (note >> (quad < 2 ? 0 : kSecondPage)) & kKeysMask ? 0xffffffffu : 0u;
 #pragma unroll 1
         for (uint32_t c = group; c < kColBlocks; c += 2) {
           if (quad == 0 && lane == 0) AMLA_STAMP(prm, part, 0, tiles * 9 + c);
@@ -602,7 +604,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           }
           hand_over(bar(C::X_KFULL) + 8 * buf);
         }
-      } while (pages_done());
+      } while (tile_done());
     } else {
       // ---- V: lanes = its columns, 16 keys a chunk.  A thread (g = lane / 4, q = lane % 4) takes columns 128 quad + 16 g .., one group with one scale, of
       // four keys: words of two keys are interleaved by nibbles and converted, which gives pairs of keys.  Column i of the sixteen goes to
@@ -620,16 +622,14 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       }
       const uint32_t pick = (g & 3) | ((4 + (g & 3)) << 4);     // this thread's group, of the four that a scale word holds, of either key
       do {
-        if (!pages_here()) break;
-        // a tile of one page has no keys in the second: its chunks are made of the first page's codes, with scales of zero
-        const int count0 = said & kKeysMask, count1 = said & kTwoPages ? said1 & kKeysMask : 0;
+        if (!tile_here()) break;
+        if (quad == 0 && lane == 0) AMLA_STAMP(prm, part, 19, tiles);
+        uint32_t codes[4], scales[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { codes[e] = code_of[e] + slot * kTileBytes; scales[e] = scale_of[e] + slot * kTileBytes; }
 #pragma unroll 1
         for (uint32_t h = 0; h < 2; ++h) {                    // page
-          const uint32_t page = (h != 0 ? slot1 : slot) * kPageBytes4;
-          const int count = (h != 0 ? count1 : count0) - 16 * static_cast<int>(group);
-          uint32_t codes[4], scales[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { codes[e] = code_of[e] + page; scales[e] = scale_of[e] + page; }
+          const int count = static_cast<int>((note >> (h * kSecondPage)) & kKeysMask) - 16 * static_cast<int>(group);   // keys that count
 #pragma unroll
           for (int i = 0; i < 2; ++i) {                       // chunk 4 h + 2 i + group
             if (quad == 0 && lane == 0) AMLA_STAMP(prm, part, 13, tiles * 8 + 4 * h + 2 * i + group);
@@ -669,8 +669,10 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
             }
             hand_over(bar(C::X_VFULL) + 8 * buf);
           }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { codes[e] += kPageBytes4; scales[e] += kPageBytes4; }
         }
-      } while (pages_done());
+      } while (tile_done());
     }
     if (!ok && lane == 0) report_timeout(prm.status);
   } else {
@@ -695,7 +697,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
             constexpr int kB = C::kKBufs;
             ok &= mbar_wait_inline(bar(C::X_KFULL + c % kB), par ^ ((c / kB) & 1));
             if (c == 0) {
-              note = ld_shared_b32(smem_base + C::kOffTiles + 4 * (gs % kUnitNotes));
+              note = ld_shared_b32(smem_base + C::kOffNotes + 8 * (gs % kNotes));
               if (note & kFirstTile) { ok &= mbar_wait_inline(bar(C::X_QREADY + un % kUnitsAhead), (un / kUnitsAhead) & 1); ++un; }
             }
             tc_fence_after_sync();
@@ -707,7 +709,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           }
           mma_commit(bar(C::X_SFULL) + 8 * sb);
           ++gs;
-          more = ok && !(note & kNoMoreTiles);
+          more = ok && !(note & kLastTile);
         }
         if (!ok) report_timeout(prm.status);
       }
@@ -727,7 +729,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           for (int c = 0; c < kVChunks; ++c) {
             constexpr int kB = C::kVBufs;
             ok &= mbar_wait_inline(bar(C::X_VFULL + c % kB), (c / kB) & 1);
-            if (c == 0) note = ld_shared_b32(smem_base + C::kOffTiles + 4 * (gp % kUnitNotes));
+            if (c == 0) note = ld_shared_b32(smem_base + C::kOffNotes + 8 * (gp % kNotes));
             tc_fence_after_sync();                            // (V, and at first P~; O may have been rescaled)
             AMLA_STAMP(prm, part, 17, gp * 8 + c);
             const uint32_t a = C::kVCol + 32 * (c % kB), pc = pl + c * (16 * 128 >> 4);
@@ -742,7 +744,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           }
           mma_commit(bar(C::X_PVDONE));
           ++gp;
-          more = ok && !(note & kNoMoreTiles);
+          more = ok && !(note & kLastTile);
         }
         if (!ok) report_timeout(prm.status);
       }
@@ -751,39 +753,54 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
     // ======================================================== pages in order
     if (elect_one()) {
       Tiles tile(UnitIter(prm, prefix, seqlens, part), first);
-      uint32_t slot = 0, par = 1, n_issued = 0, un = 0, tiles = 0;
-      int i = 0;                                            // page of the tile
-      auto entry = [&]() { return __ldg(prm.block_table + static_cast<size_t>(tile.u.b) * prm.max_blocks_per_seq + tile.t + i); };
-      auto note_unit = [&]() { st_shared_v4(smem_base + C::kOffUnits + (un++ % kUnitNotes) * 16, tile.u.b, tile.u.r0, tile.valid ? tile.u.n_b : 0, 0); };
+      uint32_t slot = 0, par = 1, n_issued = 0, un = 0;
+      auto note_unit = [&]() {
+        const uint32_t at = smem_base + C::kOffUnits + (un++ % kNotes) * 32;
+        st_shared_v4(at, tile.u.b, tile.u.r0, tile.valid ? tile.u.n_b : 0, 0);
+        if (!tile.valid) return;
+        int2 info;
+        const int pslot = tile.units.slot_of(tile.u, &info);
+        st_shared_v4(at + 16, pslot, tile.u.it, info.x, info.y);
+      };
       note_unit();
       mbar_arrive(bar(C::X_START));
-      int page = tile.valid ? entry() : 0;
-      for (bool any = tile.valid; any;) {
-        const int here = page;
+      int page[2] = {0, 0};                                 // the next tile's
+      auto look_up = [&]() {
+        const int32_t* entry = prm.block_table + static_cast<size_t>(tile.u.b) * prm.max_blocks_per_seq + tile.t;
+        page[0] = __ldg(entry);
+        if (tile.np == 2) page[1] = __ldg(entry + 1);
+      };
+      if (tile.valid) look_up();
+      while (tile.valid) {
         const bool opens = tile.first;
-        if (opens && i == 0 && n_issued > 0) {
+        const int np = tile.np, here[2] = {page[0], page[1]};
+        const uint32_t key0 = tile.t * kPage;
+        uint32_t note = (opens ? kFirstTile : 0) | (np == 2 ? kTwoPages : 0), bytes = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (i < np && here[i] >= 0 && here[i] < prm.num_blocks) {
+            note |= static_cast<uint32_t>(min(kPage, tile.u.n_b - (tile.t + i) * kPage)) << (i * kSecondPage);
+            bytes += kPageBytes4;
+          }
+        if (opens && n_issued > 0) {
           note_unit();
           // a unit's Q is asked for by the warps that widen K, when that of the unit before is done with: bring it near
           const size_t row = static_cast<size_t>(tile.u.b) * prm.R + tile.u.r0;
           bulk_prefetch_l2(prm.q + row * kDqk, static_cast<uint32_t>(min(kN, prm.R - tile.u.r0)) * (kDqk * 2));
         }
-        uint32_t say = (tile.np == 2 ? kTwoPages : 0) | (opens ? kFirstTile : 0);
-        if (here >= 0 && here < prm.num_blocks) say |= static_cast<uint32_t>(min(kPage, tile.u.n_b - (tile.t + i) * kPage));
-        bool last_page = false;
-        if (++i == tile.np) { i = 0; last_page = true; tile.next(); }
-        if (tile.valid) page = entry();                     // on its way while this page waits for its slot
-        any = tile.valid;
+        tile.next();
+        if (tile.valid) look_up();                          // on its way while this tile waits for its slot
+        if (!tile.valid) note |= kLastTile;
+        if (!tile.valid || tile.first) note |= kEndsUnit;
         ok = mbar_wait_inline(bar(C::X_EMPTY) + 8 * slot, par);
         if (!ok) break;
-        if (last_page) st_shared_b32(smem_base + C::kOffTiles + 4 * (tiles++ % kUnitNotes), (opens ? kFirstTile : 0) | (any ? 0 : kNoMoreTiles));
         const uint32_t full = bar(C::X_FULL) + 8 * slot;
-        st_shared_b32(smem_base + C::kOffInfo + 4 * slot, say | (any ? 0 : kNoMoreTiles));
-        if ((say & kKeysMask) != 0) {
-          mbar_arrive_expect_tx(full, kPageBytes4);
-          bulk_load(smem_base + C::kOffRaw + slot * kPageBytes4, prm.kv4 + static_cast<size_t>(here) * kPageBytes4, kPageBytes4, full);
-        } else {
-          mbar_arrive(full);
-        }
+        st_shared_v2(smem_base + C::kOffNotes + 8 * (n_issued % kNotes), note, key0);
+        if (bytes != 0) mbar_arrive_expect_tx(full, bytes); else mbar_arrive(full);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if ((note >> (i * kSecondPage)) & kKeysMask)
+            bulk_load(smem_base + C::kOffRaw + slot * kTileBytes + i * kPageBytes4, prm.kv4 + static_cast<size_t>(here[i]) * kPageBytes4, kPageBytes4, full);
         ++n_issued;
         if (++slot == C::kSlots) { slot = 0; par ^= 1; }
       }
