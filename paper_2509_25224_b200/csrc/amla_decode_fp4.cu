@@ -60,7 +60,7 @@ struct Shape {
   static constexpr int kThreads = 32 * (kQkWarp + 4);
   // Registers a thread, by warpgroup: together what the block is launched with
   static constexpr int kLaunchRegs = 65536 / kThreads / 8 * 8;
-  static constexpr int kSoftmaxRegs = kN == 64 ? 112 : 136, kWidenRegs = kN == 64 ? 56 : 72, kIssueRegs = 56;
+  static constexpr int kSoftmaxRegs = kN == 64 ? 104 : 136, kWidenRegs = kN == 64 ? 64 : 72, kIssueRegs = kN == 64 ? 40 : 56;
   static_assert(kGroups * kSoftmaxRegs + 4 * kWidenRegs + kIssueRegs <= kThreads / 128 * kLaunchRegs, "the block has no more to give out");
   static constexpr int kSlots = kN == 64 ? 3 : 4;       // tiles (two pages) in shared memory
   // Operand chunks in tensor memory, of K and of V: numbers that divide a tile's, so that a tile's chunks always have the same places.
@@ -202,7 +202,14 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
   if (wid == C::kQkWarp) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
   if (plan_here) {
     if (by_warp) __syncwarp(); else __syncthreads();
-    if (wid == kLoadWarp) plan_units(prm, plan_smem, lens_smem, first_smem, part, lane);
+    if (wid == kLoadWarp) {
+      plan_units(prm, plan_smem, lens_smem, first_smem, part, lane);
+      __syncwarp();
+      // the first unit's Q on its way (into L2, where it is coherent: the guess may be wrong, and Q may still be written)
+      const Unit& u = first_smem->u;
+      if (lane == 0 && u.t1 > u.t0)
+        bulk_prefetch_l2(prm.q + (static_cast<size_t>(u.b) * prm.R + u.r0) * kDqk, static_cast<uint32_t>(min(kN, prm.R - u.r0)) * (kDqk * 2));
+    }
   }
   if (tid == 0) AMLA_STAMP(prm, part, 20, 1);
   tc_fence_before_sync();
@@ -437,20 +444,21 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       const int last = pslot < 0 ? rows : kCols;
       const bool b0 = lane & 8, b1 = lane & 16;
       dst += 128 * quad + 16 * (lane & 7) + static_cast<size_t>(lane >> 3) * kDv;
+      // (Four rows at a time in a loop that stays rolled: it is run through once, and what costs is to fetch its code.)
 #pragma unroll 1
-      for (int i = 0; i < kCols / 16 * 2; ++i) {
-        const int p = i & 1, rb = (i >> 1) * 16;
-        uint32_t lo[16], hi[16];
-        tmem_ld_32x32b_x16(o_addr + kN * (2 * p) + rb, lo);
-        tmem_ld_32x32b_x16(o_addr + kN * (2 * p + 1) + rb, hi);
-        tmem_wait_ld();
+      for (int j = 0; j < kCols; j += 4) {
+        uint32_t o[4][4], f[4];
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-          uint32_t a[4], f[4];
-          ld_shared_v4(add + 4 * (rb + j), f[0], f[1], f[2], f[3]);
+        for (int m = 0; m < 4; ++m) tmem_ld_32x32b_x4(o_addr + kN * m + j, o[m]);
+        ld_shared_v4(add + 4 * j, f[0], f[1], f[2], f[3]);
+        tmem_wait_ld();
+        const int row = j + (lane >> 3);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {                                  // blocks 2p, 2p + 1
+          uint32_t a[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const float x = __uint_as_float(lo[j + c]) * __uint_as_float(f[c]), z = __uint_as_float(hi[j + c]) * __uint_as_float(f[c]);
+            const float x = __uint_as_float(o[2 * p][c]) * __uint_as_float(f[c]), z = __uint_as_float(o[2 * p + 1][c]) * __uint_as_float(f[c]);
             a[c] = pslot < 0 ? pack_bf16x2(x, z) : pack_f16x2(x, z);
           }
           const uint32_t g0 = __shfl_xor_sync(0xffffffffu, b1 ? a[0] : a[2], 16), g1 = __shfl_xor_sync(0xffffffffu, b1 ? a[1] : a[3], 16);
@@ -459,10 +467,10 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           const uint32_t kk = b0 ? k1 : k0, kg = b0 ? g1 : g0;                        // row 2 b1 + b0 from lanes L, L ^ 16, L ^ 8 (t0), L ^ 24 (t1)
           const uint32_t m0 = b0 ? t0 : kk, m1 = b0 ? kk : t0, n0 = b0 ? t1 : kg, n1 = b0 ? kg : t1;
           const uint32_t c0 = b1 ? n0 : m0, c1 = b1 ? n1 : m1, c2 = b1 ? m0 : n0, c3 = b1 ? m1 : n1;   // columns (i, i + 4)
-          const int row = rb + j + (lane >> 3);
           if (row < last)
-            stg_128(dst + static_cast<size_t>(rb + j) * kDv + 8 * p, __byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410), __byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
+            stg_128(dst + 8 * p, __byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410), __byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
         }
+        dst += 4 * kDv;
       }
       if (tid == 0) AMLA_STAMP(prm, part, 12, un);
       tc_fence_before_sync();      // O has been read: this warp's next PREADY arrival lets the next unit overwrite it
