@@ -295,7 +295,10 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
             ld_shared_v4(mult + 4 * r, m[0], m[1], m[2], m[3]);
             ld_shared_v4(neg + 4 * r, n[0], n[1], n[2], n[3]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[r + i] = fmaf(__uint_as_float(s[r + i]), __uint_as_float(m[i]), __uint_as_float(n[i]));
+            for (int i = 0; i < 4; i += 2)
+              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[r + i]), __uint_as_float(s[r + i + 1])), pack_f32x2(__uint_as_float(m[i]), __uint_as_float(m[i + 1])),
+                                     pack_f32x2(__uint_as_float(n[i]), __uint_as_float(n[i + 1]))),
+                           y[r + i], y[r + i + 1]);
           }
         }
         uint32_t key0;
@@ -382,8 +385,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
 #pragma unroll
         for (int r = 0; r < kCols; r += 2) {
           const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
-          l[r] += p0;
-          l[r + 1] += p1;
+          unpack_f32x2(add_f32x2(pack_f32x2(l[r], l[r + 1]), pack_f32x2(p0, p1)), l[r], l[r + 1]);
           pk[r / 2] = pack_f16x2(p0, p1);
         }
         if (tid == 0) AMLA_STAMP(prm, part, 9, gs);
@@ -485,10 +487,11 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
     const uint32_t raw = smem_base + C::kOffRaw, lanes = tbase + (static_cast<uint32_t>(quad * 32) << 16);
     const uint32_t group = ((wid - C::kKWarp) >> 2) & 1;     // of the two that take turns by chunk
     uint32_t slot = 0, par = 0, tiles = 0, note = 0;
+    int left = kWaitTries;
     auto tile_here = [&]() {                                 // false: the wait ran out
-      ok &= mbar_wait_inline(bar(C::X_FULL) + 8 * slot, par);
+      mbar_wait_spend(bar(C::X_FULL) + 8 * slot, par, left);
       note = ld_shared_b32(smem_base + C::kOffNotes + 8 * (tiles % kNotes));
-      ok = __all_sync(0xffffffffu, ok);
+      ok = __all_sync(0xffffffffu, left > 0);
       return ok;
     };
     auto tile_done = [&]() {                                 // (what was read of it is in registers)
@@ -499,7 +502,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       return ok && !(note & kLastTile);
     };
     auto place = [&](uint32_t empty, uint32_t use) {
-      ok &= mbar_wait_inline(empty, (use & 1) ^ 1);
+      mbar_wait_spend(empty, (use & 1) ^ 1, left);
       __syncwarp();
       tc_fence_after_sync();
     };
@@ -530,22 +533,27 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       cp_async_wait_all();
 #pragma unroll 1
       for (int r = r0; r < r0 + each; ++r) {              // (a thread converts what it has brought itself)
-        uint32_t x[3][4], top = 0;
+        uint32_t x[3][4], top = 0;                           // the largest magnitude, of either half of the words, as integers
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
           x[j][0] = x[j][1] = x[j][2] = x[j][3] = 0;
           if (j < 2 || lane < 8) ld_shared_v4(piece(r, j), x[j][0], x[j][1], x[j][2], x[j][3]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) top = max(top, max((x[j][c] << 16) & 0x7fffffffu, x[j][c] & 0x7fff0000u));
+          top = __vimax3_u16x2(top, x[j][0] & 0x7fff7fffu, x[j][1] & 0x7fff7fffu);
+          top = __vimax3_u16x2(top, x[j][2] & 0x7fff7fffu, x[j][3] & 0x7fff7fffu);
         }
-        const uint32_t e = __reduce_max_sync(0xffffffffu, top) >> 23;
+        const uint32_t e = __reduce_max_sync(0xffffffffu, max(top >> 16, top & 0xffffu)) >> 7;
         // 2^(14 - (e - 127)) and its inverse; the largest powers that FP32 has for rows below 2^-113, 1 for rows that are not finite
         const float up = e == 255 ? 1.f : __uint_as_float(e <= 14 ? 254u << 23 : (268u - e) << 23);
         const float down = e == 255 ? 1.f : __uint_as_float(e <= 14 ? 0x00400000u : (e - 14u) << 23);
+        const uint64_t up2 = pack_f32x2(up, up);
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) x[j][c] = pack_f16x2(__uint_as_float(x[j][c] << 16) * up, __uint_as_float(x[j][c] & 0xffff0000u) * up);
+          for (int c = 0; c < 4; ++c) {
+            float lo, hi;
+            unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(x[j][c] << 16), __uint_as_float(x[j][c] & 0xffff0000u)), up2), lo, hi);
+            x[j][c] = pack_f16x2(lo, hi);
+          }
           if (j < 2 || lane < 8) st_shared_v4(piece(r, j), x[j][0], x[j][1], x[j][2], x[j][3]);
         }
         if (lane == 0) {
@@ -692,21 +700,22 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       if (elect_one()) {
         constexpr uint32_t idesc = make_idesc_f16(128, kN, false, false);
         uint32_t gs = 0, un = 0;
+        int left = kWaitTries;
         ok = mbar_wait_inline(bar(C::X_START), 0);
         bool more = ok && static_cast<int>(ld_shared_b32(smem_base + C::kOffUnits + 8)) > 0;
         while (more) {
           const uint32_t sb = gs % C::kSBufs, d = C::kSCol + sb * kN, par = gs & 1;      // (nine chunks in three places: an odd number of rounds)
-          ok &= mbar_wait_inline(bar(C::X_SEMPTY) + 8 * sb, ((gs / C::kSBufs) & 1) ^ 1);
+          mbar_wait_spend(bar(C::X_SEMPTY) + 8 * sb, ((gs / C::kSBufs) & 1) ^ 1, left);
           constexpr uint32_t kQStep = C::kQBlock >> 4;
           const uint32_t ql = smem_desc_lo(smem_base, 16);
           uint32_t note = 0;
 #pragma unroll
           for (int c = 0; c < kColBlocks; ++c) {
             constexpr int kB = C::kKBufs;
-            ok &= mbar_wait_inline(bar(C::X_KFULL + c % kB), par ^ ((c / kB) & 1));
+            mbar_wait_spend(bar(C::X_KFULL + c % kB), par ^ ((c / kB) & 1), left);
             if (c == 0) {
               note = ld_shared_b32(smem_base + C::kOffNotes + 8 * (gs % kNotes));
-              if (note & kFirstTile) { ok &= mbar_wait_inline(bar(C::X_QREADY + un % kUnitsAhead), (un / kUnitsAhead) & 1); ++un; }
+              if (note & kFirstTile) { mbar_wait_spend(bar(C::X_QREADY + un % kUnitsAhead), (un / kUnitsAhead) & 1, left); ++un; }
             }
             tc_fence_after_sync();
             AMLA_STAMP(prm, part, 5, gs * 9 + c);
@@ -717,6 +726,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           }
           mma_commit(bar(C::X_SFULL) + 8 * sb);
           ++gs;
+          ok = left > 0;
           more = ok && !(note & kLastTile);
         }
         if (!ok) report_timeout(prm.status);
@@ -727,16 +737,17 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       if (elect_one()) {
         constexpr uint32_t idesc = make_idesc_f16(128, kN, false, true);
         uint32_t gp = 0;
+        int left = kWaitTries;
         ok = mbar_wait_inline(bar(C::X_START), 0);
         bool more = ok && static_cast<int>(ld_shared_b32(smem_base + C::kOffUnits + 8)) > 0;
         while (more) {
-          ok &= mbar_wait_inline(bar(C::X_PREADY), gp & 1);
+          mbar_wait_spend(bar(C::X_PREADY), gp & 1, left);
           const uint32_t pl = smem_desc_lo(smem_base + C::kOffP, 16);
           uint32_t note = 0;
 #pragma unroll
           for (int c = 0; c < kVChunks; ++c) {
             constexpr int kB = C::kVBufs;
-            ok &= mbar_wait_inline(bar(C::X_VFULL + c % kB), (c / kB) & 1);
+            mbar_wait_spend(bar(C::X_VFULL + c % kB), (c / kB) & 1, left);
             if (c == 0) note = ld_shared_b32(smem_base + C::kOffNotes + 8 * (gp % kNotes));
             tc_fence_after_sync();                            // (V, and at first P~; O may have been rescaled)
             AMLA_STAMP(prm, part, 17, gp * 8 + c);
@@ -752,6 +763,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           }
           mma_commit(bar(C::X_PVDONE));
           ++gp;
+          ok = left > 0;
           more = ok && !(note & kLastTile);
         }
         if (!ok) report_timeout(prm.status);

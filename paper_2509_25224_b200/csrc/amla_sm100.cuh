@@ -116,22 +116,24 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_
 }
 
 // The same as one piece of code that runs straight through when the phase is complete, for kernels that cannot have calls in them
-// (setmaxnreg) and for loops where a taken branch (some 30 clk) counts.  It gives up after kWaitTries tries, of 20 clk at least and
-// of as long as the hardware suspends a thread otherwise: 45 ms or more.
-constexpr uint32_t kWaitTries = 1u << 22, kWaitHintNs = 1000;
-__device__ __forceinline__ bool mbar_wait_inline(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
+// (setmaxnreg) and for loops where every instruction counts.  `left` is what the thread may still spend on waits that did not succeed at
+// once, kWaitTries tries at first; when it is used up (0) waits no longer wait, and who looks at it now and then gives up.  (A try takes 20 clk
+// at least and as long as the hardware suspends a thread otherwise, 5 us as measured: 80 ms or more.)
+constexpr int kWaitTries = 1 << 22;
+__device__ __forceinline__ void mbar_wait_spend(uint32_t bar, uint32_t parity, int& left) {
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
-      "mov.u32 n, %3;\n"
+      "{\n\t.reg .pred p, q;\n"
       "L_TRY_%=:\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %4;\n\t"
-      "sub.u32 n, n, 1;\n\t"
-      "setp.ne.and.u32 q, n, 0, !p;\n\t"
-      "@q bra L_TRY_%=;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(bar), "r"(parity), "n"(kWaitTries), "n"(kWaitHintNs) : "memory");
-  return ok != 0;
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "@!p sub.s32 %0, %0, 1;\n\t"
+      "setp.gt.and.s32 q, %0, 0, !p;\n\t"
+      "@q bra L_TRY_%=;\n\t}"
+      : "+r"(left) : "r"(bar), "r"(parity), "n"(1000) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait_inline(uint32_t bar, uint32_t parity) {
+  int left = kWaitTries;
+  mbar_wait_spend(bar, parity, left);
+  return left > 0;
 }
 // Arrives where `yes` (no branch around it, so that a warp stays together).
 __device__ __forceinline__ void mbar_arrive_if(bool yes, uint32_t bar) {
