@@ -492,6 +492,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       mbar_wait_spend(bar(C::X_FULL) + 8 * slot, par, left);
       note = ld_shared_b32(smem_base + C::kOffNotes + 8 * (tiles % kNotes));
       ok = __all_sync(0xffffffffu, left > 0);
+      left = kWaitTries;
       return ok;
     };
     auto tile_done = [&]() {                                 // (what was read of it is in registers)
@@ -499,8 +500,10 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       mbar_arrive_if(lane == 0, bar(C::X_EMPTY) + 8 * slot);
       if (++slot == C::kSlots) { slot = 0; par ^= 1; }
       ++tiles;
-      return ok && !(note & kLastTile);
+      return !(note & kLastTile);
     };
+    // (A place of K's is used by both groups by turns.  A group can still not be two phases of its barrier ahead: the products take chunks in order,
+    // and the group's own chunk before this one was placed when the one three before it had been taken.)
     auto place = [&](uint32_t empty, uint32_t use) {
       mbar_wait_spend(empty, (use & 1) ^ 1, left);
       __syncwarp();
@@ -690,6 +693,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
         }
       } while (tile_done());
     }
+    ok = __all_sync(0xffffffffu, ok && left > 0);
     if (!ok && lane == 0) report_timeout(prm.status);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
@@ -727,6 +731,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           mma_commit(bar(C::X_SFULL) + 8 * sb);
           ++gs;
           ok = left > 0;
+          left = kWaitTries;
           more = ok && !(note & kLastTile);
         }
         if (!ok) report_timeout(prm.status);
@@ -764,6 +769,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           mma_commit(bar(C::X_PVDONE));
           ++gp;
           ok = left > 0;
+          left = kWaitTries;
           more = ok && !(note & kLastTile);
         }
         if (!ok) report_timeout(prm.status);

@@ -116,10 +116,10 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_
 }
 
 // The same as one piece of code that runs straight through when the phase is complete, for kernels that cannot have calls in them
-// (setmaxnreg) and for loops where every instruction counts.  `left` is what the thread may still spend on waits that did not succeed at
-// once, kWaitTries tries at first; when it is used up (0) waits no longer wait, and who looks at it now and then gives up.  (A try takes 20 clk
-// at least and as long as the hardware suspends a thread otherwise, 5 us as measured: 80 ms or more.)
-constexpr int kWaitTries = 1 << 22;
+// (setmaxnreg) and for loops where every instruction counts.  `left` is how many tries the thread may still spend on waits that do not
+// succeed at once, kWaitTries at first; when it is used up (0) waits no longer wait, and who looks at it now and then gives up.  (The hardware
+// suspends a thread for 5 us a try, as measured, which makes it 1.3 s; at 20 clk, the least that a try takes, it would be 3 ms.)
+constexpr int kWaitTries = 1 << 18;
 __device__ __forceinline__ void mbar_wait_spend(uint32_t bar, uint32_t parity, int& left) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n"
