@@ -63,8 +63,8 @@ struct Shape {
   static constexpr int kSoftmaxRegs = kN == 64 ? 104 : 136, kWidenRegs = kN == 64 ? 64 : 72, kIssueRegs = kN == 64 ? 40 : 56;
   static_assert(kGroups * kSoftmaxRegs + 4 * kWidenRegs + kIssueRegs <= kThreads / 128 * kLaunchRegs, "the block has no more to give out");
   static constexpr int kSlots = kN == 64 ? 3 : 4;       // tiles (two pages) in shared memory
-  // Operand chunks in tensor memory, of K and of V: numbers that divide a tile's, so that a tile's chunks always have the same places.
-  static constexpr int kKBufs = 3, kVBufs = kN == 64 ? 2 : 4;
+  // Operand chunks in tensor memory, of K and of V: a tile's always have the same places, and a place is always the same group's.
+  static constexpr int kKBufs = 4, kVBufs = kN == 64 ? 2 : 4;
   static constexpr int kSBufs = kN == 64 ? 1 : 2;       // score tiles in tensor memory
   static constexpr uint32_t kQBlock = kN * 128;         // [rows][64 columns of f16], 128-byte swizzle
   static constexpr uint32_t kOffP = kColBlocks * kQBlock;
@@ -95,7 +95,6 @@ struct Shape {
   static_assert(kBytes <= 232448, "exceeds the shared memory a block can opt in to");
   static_assert(kOffP % 1024 == 0 && kOffRaw % 1024 == 0 && kTileBytes % 16 == 0 && kOffBars % 8 == 0, "alignment");
   static_assert(kSCol + kSBufs * kN <= kKCol && kSlots + 4 < kNotes, "tensor memory");
-  static_assert(kColBlocks % kKBufs == 0 && kVChunks % kVBufs == 0 && (kVBufs == 2 || kVBufs == 4), "places of chunks");
 };
 
 __device__ __forceinline__ void report_timeout(int* status) { atomicExch(status, kStatusTimeout); }
@@ -502,8 +501,6 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       ++tiles;
       return !(note & kLastTile);
     };
-    // (A place of K's is used by both groups by turns.  A group can still not be two phases of its barrier ahead: the products take chunks in order,
-    // and the group's own chunk before this one was placed when the one three before it had been taken.)
     auto place = [&](uint32_t empty, uint32_t use) {
       mbar_wait_spend(empty, (use & 1) ^ 1, left);
       __syncwarp();
@@ -605,7 +602,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           const uint32_t sw = ld_shared_b32(scales) & there;
           codes += 64;
           scales += 8;
-          const uint32_t round = (c * 11) >> 5, buf = c - 3 * round;          // c / 3, c % 3
+          const uint32_t buf = c & 3;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {                      // (half at a time: registers)
             uint32_t r[16];
@@ -618,7 +615,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
 #pragma unroll
               for (int i = 0; i < 4; ++i) r[4 * j + i] = mul_f16x2(x[i], sc[j / 2]);
             }
-            if (h == 0) place(bar(C::X_KEMPTY) + 8 * buf, tiles + round);
+            if (h == 0) place(bar(C::X_KEMPTY) + 8 * buf, (buf == 0 ? tiles : 0) + (c >> 2));      // three chunks a tile in place 0, two in the others
             tmem_st_32x32b_x16(lanes + C::kKCol + 32 * buf + 16 * h, r);
           }
           hand_over(bar(C::X_KFULL) + 8 * buf);
@@ -708,7 +705,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
         ok = mbar_wait_inline(bar(C::X_START), 0);
         bool more = ok && static_cast<int>(ld_shared_b32(smem_base + C::kOffUnits + 8)) > 0;
         while (more) {
-          const uint32_t sb = gs % C::kSBufs, d = C::kSCol + sb * kN, par = gs & 1;      // (nine chunks in three places: an odd number of rounds)
+          const uint32_t sb = gs % C::kSBufs, d = C::kSCol + sb * kN, par = gs & 1;
           mbar_wait_spend(bar(C::X_SEMPTY) + 8 * sb, ((gs / C::kSBufs) & 1) ^ 1, left);
           constexpr uint32_t kQStep = C::kQBlock >> 4;
           const uint32_t ql = smem_desc_lo(smem_base, 16);
@@ -716,7 +713,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
 #pragma unroll
           for (int c = 0; c < kColBlocks; ++c) {
             constexpr int kB = C::kKBufs;
-            mbar_wait_spend(bar(C::X_KFULL + c % kB), par ^ ((c / kB) & 1), left);
+            mbar_wait_spend(bar(C::X_KFULL + c % kB), (c % kB == 0 ? par : 0) ^ ((c / kB) & 1), left);      // (three chunks a tile in place 0, two in the others)
             if (c == 0) {
               note = ld_shared_b32(smem_base + C::kOffNotes + 8 * (gs % kNotes));
               if (note & kFirstTile) { mbar_wait_spend(bar(C::X_QREADY + un % kUnitsAhead), (un / kUnitsAhead) & 1, left); ++un; }
