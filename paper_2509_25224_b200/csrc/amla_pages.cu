@@ -5,6 +5,10 @@
 // free, fork, reserve and compact follow one rule: pages are handed out lowest first, in the order of the requests.  That is a rank
 // among the free pages (or, to compact, among those in use), which blocks of a grid find from one another's totals: a launch
 // counts by chunks of kChunk pages, the next adds the totals up in front of its chunk.  Up to kChunk pages the first launch is left out.
+//
+// What bounds them: the books are some kilobytes, so that free, fork, reserve and a compaction that finds nothing to move cost their launches
+// and a few dependent reads (1.3, 3.6, 2.8 and 8.2 us in a graph, 64 rows of 128 entries and 8192 pages); copies are bound by the
+// memory, which takes 16 bytes a thread four deep at full occupancy: 8 192 pages of 20 736 bytes move at the rate of a plain copy.
 #include <algorithm>
 
 #include "../../include/amla.h"
@@ -21,6 +25,12 @@ constexpr int kRowThreads = 256;
 constexpr int kCopyThreads = 256;
 constexpr int kCopyUnroll = 4;
 constexpr int kSegment = kCopyThreads * kCopyUnroll; // 16-byte pieces that a block copies at a time
+// Blocks that move pages.  How many there are to move is only known on the device, so that a block takes every kMoveBlocks-th piece
+// of the work.  9 948 moves of 20 736 bytes (412 MB), with the launches in front and the events' own 5 us: 87 us with the eight
+// blocks that an SM holds (the second segment of a page is short, and a block has always the one kind or the other), 79 with four
+// times as many, which are dealt out as others end, 97 with one for every piece that there might be.  (A compaction of 8192 pages that
+// finds nothing to move: 4.2, 8.2.)
+constexpr int kMoveBlocks = 148 * 32;
 constexpr size_t kAlign = 256;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -240,6 +250,51 @@ __global__ void __launch_bounds__(kCopyThreads) fork_rows_kernel(uint4* __restri
   }
 }
 
+// The whole of it by one block, for a cache of at most kChunk pages: the free pages are listed in shared memory, a thread serves a
+// row's first page and its books, the warp the others.  (64 rows, 8192 pages: 2.7 us, and 7 us of the host; as the two launches that
+// larger caches take 3.1 us, and 13.)
+__global__ void __launch_bounds__(kScanThreads) reserve_small_kernel(int32_t* __restrict__ block_table, int32_t* seqlens, int32_t* __restrict__ refs, int num_blocks, const Requests q,
+                                                                     int32_t* __restrict__ granted) {
+  __shared__ int list[kChunk];
+  begin();
+  const int tid = threadIdx.x, lane = tid & 31;
+  uint32_t there;
+  const uint32_t used = used_bits(refs, num_blocks, tid * kPerThread, &there);
+  uint32_t open = there & ~used;
+  int pages;
+  int at = block_scan<kScanThreads>(__popc(open), &pages);
+  for (; open != 0; open &= open - 1) list[at++] = tid * kPerThread + __ffs(open) - 1;
+  __syncthreads();
+  long long front = 0;
+  for (int row0 = 0; row0 < q.B; row0 += kScanThreads) {
+    const int row = row0 + tid;
+    const bool mine = row < q.B;
+    const int now = mine ? length_of(q.seqlens, row, q.width) : 0, then = mine ? q.new_lens[row] : 0, more = mine ? reserve_asks(q, row) : 0;
+    long long all;
+    const long long before = front + block_scan<kScanThreads, long long>(more, &all);
+    front += all;
+    const bool ok = then <= q.width * kPage && (more == 0 || before + more <= pages);
+    const int rank = ok ? static_cast<int>(before) : 0;
+    const size_t entry = static_cast<size_t>(mine ? row : 0) * q.width + pages_of(now);
+    if (ok && more > 0) {
+      const int page = list[rank];
+      block_table[entry] = page;
+      refs[page] = 1;
+    }
+    if (mine && ok && then > now) seqlens[row] = then;
+    if (mine && granted) granted[row] = ok ? 1 : 0;
+    for (uint32_t todo = __ballot_sync(0xffffffffu, ok && more > 1); todo != 0; todo &= todo - 1) {
+      const int who = __ffs(todo) - 1, count = __shfl_sync(0xffffffffu, more, who), first = __shfl_sync(0xffffffffu, rank, who);
+      const size_t to = __shfl_sync(0xffffffffu, static_cast<unsigned long long>(entry), who);
+      for (int i = 1 + lane; i < count; i += 32) {
+        const int page = list[first + i];
+        block_table[to + i] = page;
+        refs[page] = 1;
+      }
+    }
+  }
+}
+
 // One block per row.
 __global__ void __launch_bounds__(kRowThreads) reserve_rows_kernel(int32_t* __restrict__ block_table, int32_t* seqlens, int32_t* __restrict__ refs, const Requests q,
                                                                    const int* __restrict__ head, const int* __restrict__ list, const int* __restrict__ row_rank,
@@ -443,9 +498,10 @@ extern "C" int amla_pages_reserve(int32_t* block_table, int32_t* seqlens, int32_
   if (!new_lens || odd_int(new_lens) || odd_int(granted) || new_lens == seqlens) return AMLA_ERR_INVALID_ARG;
   rc = check_workspace(workspace, workspace_bytes, num_blocks, B);
   if (rc != AMLA_OK) return rc;
-  const Scratch s = carve(workspace, num_blocks);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const Requests q{seqlens, nullptr, nullptr, new_lens, B, B, max_blocks_per_seq};
+  if (chunks_of(num_blocks) == 1) return done(launch(reserve_small_kernel, dim3(1), kScanThreads, stream, block_table, seqlens, refs, num_blocks, q, granted));
+  const Scratch s = carve(workspace, num_blocks);
   const cudaError_t err = list_free(refs, num_blocks, static_cast<long long>(B) * max_blocks_per_seq, q, s, stream);
   if (err != cudaSuccess) return done(err);
   return done(launch(reserve_rows_kernel, dim3(B), kRowThreads, stream, block_table, seqlens, refs, q, s.head, s.list, s.row_rank, granted));
@@ -469,6 +525,6 @@ extern "C" int amla_pages_compact(void* cache, long long page_bytes, int32_t* bl
   if (err != cudaSuccess) return done(err);
   const int pieces = static_cast<int>(page_bytes / 16), segments = (pieces + kSegment - 1) / kSegment;
   const long long most = std::max<long long>(static_cast<long long>(num_blocks / 2 + 1) * segments, (static_cast<long long>(B) * max_blocks_per_seq + kCopyThreads - 1) / kCopyThreads);
-  return done(launch(move_pages_kernel, dim3(static_cast<int>(std::min<long long>(most, 148 * 8))), kCopyThreads, stream, static_cast<uint4*>(cache), pieces, block_table, seqlens, refs, B,
+  return done(launch(move_pages_kernel, dim3(static_cast<int>(std::min<long long>(most, kMoveBlocks))), kCopyThreads, stream, static_cast<uint4*>(cache), pieces, block_table, seqlens, refs, B,
                      num_blocks, max_blocks_per_seq, s.head, s.list, s.list2, s.rank));
 }
