@@ -93,7 +93,7 @@ constexpr int kQuadOverheadTiles = AMLA_QUAD_OVERHEAD_TILES;
 #endif
 constexpr int kFewOverheadTiles = AMLA_FEW_OVERHEAD_TILES;
 #ifndef AMLA_FP4_OVERHEAD_TILES
-#define AMLA_FP4_OVERHEAD_TILES 4             // kernel for a 4-bit cache: in 64-key pages
+#define AMLA_FP4_OVERHEAD_TILES 5             // kernel for a 4-bit cache: in 64-key pages (3 and 4 take 3 to 12 % longer with 48 ragged sequences of 64 heads, 6 and 7 4 % with 32 x 4096 of 128)
 #endif
 constexpr int kFp4OverheadTiles = AMLA_FP4_OVERHEAD_TILES;
 constexpr int kMinPartKeys = 128;           // a part holds at least this many keys: a shorter one takes as long, and every part is a partial to merge
