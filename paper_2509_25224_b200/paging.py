@@ -16,17 +16,28 @@ from .binding import AMLA_OK, AmlaError
 
 FP4_PAGE_BYTES = binding._FP4_PAGE_SHAPE[0]
 
-_torch = None
+_torch = _int = None
 _sizes: dict = {}                    # workspace bytes by (num_blocks, B)
 
 
 def _ready():
-    """torch and the loaded library."""
-    global _torch
-    if _torch is None:
+    """The loaded library (and torch, for the checks)."""
+    global _torch, _int
+    if _int is None:
         import torch
-        _torch = torch
-    return _torch, binding._lib if binding._lib is not None else binding.lib()
+        _torch, _int = torch, torch.int32
+    return binding._lib if binding._lib is not None else binding.lib()
+
+
+def _call(on, entry, args, what):
+    """entry(*args, stream) on the current stream of device `on`.  (Where that is the current device, which is cheap to ask for once a tensor of
+    it exists, without the wrappers that binding._on_device has; 0.5 us of a call that takes 7.)"""
+    if on == _torch._C._cuda_getDevice():
+        rc = entry(*args, _torch._C._cuda_getCurrentRawStream(on))
+        if rc != AMLA_OK:
+            raise AmlaError(rc, what)
+    else:
+        binding._on_device(_torch.device("cuda", on), entry, args, (), what)
 
 
 def workspace_size(num_blocks: int, B: int) -> int:
@@ -39,7 +50,7 @@ def workspace_size(num_blocks: int, B: int) -> int:
 
 
 def _int32(t, on, name):
-    if t.dtype is not _torch.int32 or not t.is_contiguous() or t.get_device() != on:
+    if t.dtype is not _int or not t.is_contiguous() or t.get_device() != on:
         raise ValueError(name + " must be a contiguous int32 tensor on the device of the others")
 
 
@@ -67,7 +78,7 @@ def _page_bytes(cache, on=None, num_blocks=None):
     return cache.numel() // blocks * cache.element_size()
 
 
-def _scratch(workspace, num_blocks, B, on, device):
+def _scratch(workspace, num_blocks, B, on, like):
     """(tensor, bytes); the tensor is the caller's, or one that lives until the call is enqueued (the allocator keeps the stream's order)."""
     if workspace is None:
         key = (num_blocks, B)
@@ -76,15 +87,15 @@ def _scratch(workspace, num_blocks, B, on, device):
             if len(_sizes) > 64:
                 _sizes.clear()
             size = _sizes[key] = workspace_size(num_blocks, B)
-        return _torch.empty(size, dtype=_torch.uint8, device=device), size
+        return like.new_empty((size + 3) // 4), size
     if workspace.get_device() != on or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the device of the others")
     return workspace, workspace.numel() * workspace.element_size()
 
 
-def _answers(t, n, on, device, name):
+def _answers(t, n, on, like, name):
     if t is None:
-        return _torch.empty(n, dtype=_torch.int32, device=device)
+        return like.new_empty(n)
     _int32(t, on, name)
     if t.dim() != 1 or t.numel() != n:
         raise ValueError("%s must be [%d]" % (name, n))
@@ -92,11 +103,12 @@ def _answers(t, n, on, device, name):
 
 
 def _tokens(rows, starts, cache, block_table, seqlens):
-    """(sequences, entries a row, pages, tokens, elements from one token to the next)"""
+    """(device index, sequences, entries a row, pages, tokens, elements from one token to the next)"""
     on = cache.get_device()
     if on < 0:
         raise ValueError("paging works on CUDA tensors, not tensors on " + str(cache.device))
-    if cache.dtype is not _torch.uint8 or cache.dim() != 2 or not cache.is_contiguous() or cache.shape[1] != FP4_PAGE_BYTES:
+    shape = cache.shape
+    if cache.dtype is not _torch.uint8 or len(shape) != 2 or shape[1] != FP4_PAGE_BYTES or not cache.is_contiguous():
         raise ValueError("the cache must be contiguous uint8 [num_blocks, %d]" % FP4_PAGE_BYTES)
     _int32(starts, on, "starts")
     _int32(block_table, on, "block_table")
@@ -116,55 +128,55 @@ def _tokens(rows, starts, cache, block_table, seqlens):
         step = 576
     elif step < 576:
         raise ValueError("rows of tokens must not overlap")
-    return B, width, cache.shape[0], n, step
+    return on, B, width, shape[0], n, step
 
 
 def cache_store_fp4(kv, starts, kv_cache_fp4, kv_scale: float, block_table, seqlens) -> None:
     """Quantises tokens kv bf16 [n, 576] (rows may be a slice of wider ones) into the 4-bit cache: rows starts[b] .. starts[b+1] - 1
     are the last tokens of sequence b, whose length seqlens[b] already counts them."""
-    _, L = _ready()
-    B, width, blocks, n, step = _tokens(kv, starts, kv_cache_fp4, block_table, seqlens)
-    binding._on_device(kv_cache_fp4.device, L.amla_cache_store_fp4,
-                       (kv.data_ptr(), step, n, starts.data_ptr(), kv_cache_fp4.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), B, blocks, width),
-                       (), "amla_cache_store_fp4")
+    L = _ready()
+    on, B, width, blocks, n, step = _tokens(kv, starts, kv_cache_fp4, block_table, seqlens)
+    _call(on, L.amla_cache_store_fp4,
+          (kv.data_ptr(), step, n, starts.data_ptr(), kv_cache_fp4.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), B, blocks, width),
+          "amla_cache_store_fp4")
 
 
 def cache_load_fp4(kv_cache_fp4, kv_scale: float, block_table, seqlens, starts, out):
     """The inverse: out[starts[b] .. starts[b+1] - 1] (bf16 [n, 576]) = the last tokens of sequence b, as the decode call sees them."""
-    _, L = _ready()
-    B, width, blocks, n, step = _tokens(out, starts, kv_cache_fp4, block_table, seqlens)
-    binding._on_device(kv_cache_fp4.device, L.amla_cache_load_fp4,
-                       (kv_cache_fp4.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), starts.data_ptr(), B, blocks, width, out.data_ptr(), step, n),
-                       (), "amla_cache_load_fp4")
+    L = _ready()
+    on, B, width, blocks, n, step = _tokens(out, starts, kv_cache_fp4, block_table, seqlens)
+    _call(on, L.amla_cache_load_fp4,
+          (kv_cache_fp4.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), starts.data_ptr(), B, blocks, width, out.data_ptr(), step, n),
+          "amla_cache_load_fp4")
     return out
 
 
 def pages_copy(cache, src, dst) -> None:
     """cache[dst[i]] = cache[src[i]] for all i; a pair with an index outside the cache is skipped."""
-    _, L = _ready()
+    L = _ready()
     page_bytes = _page_bytes(cache)
     on = cache.get_device()
     _int32(src, on, "src")
     _int32(dst, on, "dst")
     if src.dim() != 1 or dst.dim() != 1 or src.numel() != dst.numel():
         raise ValueError("src and dst are lists of the same length")
-    binding._on_device(cache.device, L.amla_pages_copy, (cache.data_ptr(), page_bytes, cache.shape[0], src.data_ptr(), dst.data_ptr(), src.numel()), (), "amla_pages_copy")
+    _call(on, L.amla_pages_copy, (cache.data_ptr(), page_bytes, cache.shape[0], src.data_ptr(), dst.data_ptr(), src.numel()), "amla_pages_copy")
 
 
 def pages_free(block_table, seqlens, refs, rows) -> None:
     """The listed rows give up their pages and are left empty."""
-    _, L = _ready()
+    L = _ready()
     on, B, width, blocks = _books(block_table, seqlens, refs)
     _int32(rows, on, "rows")
     if rows.dim() != 1:
         raise ValueError("rows is a list")
-    binding._on_device(block_table.device, L.amla_pages_free,
-                       (block_table.data_ptr(), seqlens.data_ptr(), refs.data_ptr(), rows.data_ptr(), rows.numel(), B, blocks, width), (), "amla_pages_free")
+    _call(on, L.amla_pages_free,
+          (block_table.data_ptr(), seqlens.data_ptr(), refs.data_ptr(), rows.data_ptr(), rows.numel(), B, blocks, width), "amla_pages_free")
 
 
 def pages_fork(cache, block_table, seqlens, refs, parents, children, served=None, workspace=None):
     """Row children[i] becomes a copy of row parents[i] that shares its full pages.  Returns served int32 [n]: 0 where no page was left."""
-    _, L = _ready()
+    L = _ready()
     on, B, width, blocks = _books(block_table, seqlens, refs)
     page_bytes = _page_bytes(cache, on, blocks)
     _int32(parents, on, "parents")
@@ -172,40 +184,37 @@ def pages_fork(cache, block_table, seqlens, refs, parents, children, served=None
     n = parents.numel()
     if parents.dim() != 1 or children.dim() != 1 or children.numel() != n:
         raise ValueError("parents and children are lists of the same length")
-    dev = block_table.device
-    served = _answers(served, n, on, dev, "served")
-    workspace, size = _scratch(workspace, blocks, B, on, dev)
-    binding._on_device(dev, L.amla_pages_fork,
-                       (cache.data_ptr(), page_bytes, block_table.data_ptr(), seqlens.data_ptr(), refs.data_ptr(), parents.data_ptr(), children.data_ptr(), n, B, blocks, width,
-                        served.data_ptr(), workspace.data_ptr(), size), (), "amla_pages_fork")
+    served = _answers(served, n, on, refs, "served")
+    workspace, size = _scratch(workspace, blocks, B, on, refs)
+    _call(on, L.amla_pages_fork,
+          (cache.data_ptr(), page_bytes, block_table.data_ptr(), seqlens.data_ptr(), refs.data_ptr(), parents.data_ptr(), children.data_ptr(), n, B, blocks, width,
+           served.data_ptr(), workspace.data_ptr(), size), "amla_pages_fork")
     return served
 
 
 def pages_reserve(block_table, seqlens, refs, new_lens, granted=None, workspace=None):
     """Rows grow to new_lens [B], with free pages where they need them.  Returns granted int32 [B]: 0 where the row stays as it was."""
-    _, L = _ready()
+    L = _ready()
     on, B, width, blocks = _books(block_table, seqlens, refs)
     _int32(new_lens, on, "new_lens")
     if new_lens.dim() != 1 or new_lens.numel() != B:
         raise ValueError("new_lens is [B]")
-    dev = block_table.device
-    granted = _answers(granted, B, on, dev, "granted")
-    workspace, size = _scratch(workspace, blocks, B, on, dev)
-    binding._on_device(dev, L.amla_pages_reserve,
-                       (block_table.data_ptr(), seqlens.data_ptr(), refs.data_ptr(), new_lens.data_ptr(), B, blocks, width, granted.data_ptr(), workspace.data_ptr(), size),
-                       (), "amla_pages_reserve")
+    granted = _answers(granted, B, on, refs, "granted")
+    workspace, size = _scratch(workspace, blocks, B, on, refs)
+    _call(on, L.amla_pages_reserve,
+          (block_table.data_ptr(), seqlens.data_ptr(), refs.data_ptr(), new_lens.data_ptr(), B, blocks, width, granted.data_ptr(), workspace.data_ptr(), size),
+          "amla_pages_reserve")
     return granted
 
 
 def pages_compact(cache, block_table, seqlens, refs, live=None, workspace=None):
     """Moves the pages in use to the front of the cache.  Returns live int32 [1]: how many there are; the pages from there on are free."""
-    _, L = _ready()
+    L = _ready()
     on, B, width, blocks = _books(block_table, seqlens, refs)
     page_bytes = _page_bytes(cache, on, blocks)
-    dev = block_table.device
-    live = _answers(live, 1, on, dev, "live")
-    workspace, size = _scratch(workspace, blocks, B, on, dev)
-    binding._on_device(dev, L.amla_pages_compact,
-                       (cache.data_ptr(), page_bytes, block_table.data_ptr(), seqlens.data_ptr(), refs.data_ptr(), B, blocks, width, live.data_ptr(), workspace.data_ptr(), size),
-                       (), "amla_pages_compact")
+    live = _answers(live, 1, on, refs, "live")
+    workspace, size = _scratch(workspace, blocks, B, on, refs)
+    _call(on, L.amla_pages_compact,
+          (cache.data_ptr(), page_bytes, block_table.data_ptr(), seqlens.data_ptr(), refs.data_ptr(), B, blocks, width, live.data_ptr(), workspace.data_ptr(), size),
+          "amla_pages_compact")
     return live
