@@ -271,7 +271,7 @@ int amla_validate_paging_host(const int32_t* block_table, const int32_t* seqlens
 int amla_last_launch_count(void);
 
 /* Query rows per work item of the most recent decode call on this thread, which tells the kernel that ran: 32 (the kernel
- * for few rows), 128 or 256.  0 before the first call. */
+ * for few rows), 128 or 256; with a 4-bit cache 16, 32 or 64.  0 before the first call. */
 int amla_last_item_rows(void);
 
 /* Measurement aid: when enabled, every decode call

@@ -320,7 +320,7 @@ def last_launch_count() -> int:
 
 
 def last_item_rows() -> int:
-    """Query rows per work item of this thread's last decode call: 32, 128 or 256, after the kernel that ran."""
+    """Query rows per work item of this thread's last decode call: 32, 128 or 256, after the kernel that ran (4-bit cache: 16, 32 or 64)."""
     return int(lib().amla_last_item_rows())
 
 

@@ -8,8 +8,8 @@
 //   O^T += V^T P~^T   A = V^T: V's columns are the lanes, 4 x 128 of them and 16 keys at a time; B = P~ (shared memory, MN-major)
 //
 // One CTA works on up to 16, 32 or 64 rows of a sequence and a range of its pages; O^T is four blocks of kN columns of tensor
-// memory (256 for 64 rows), S^T two of kN, and the rest a ring of operand chunks of 32 columns.  A 128-key tile is 17 chunks: nine of K
-// (128 keys x 64 columns), eight of V (512 columns x 16 keys), four MMAs each.
+// memory (256 for 64 rows), S^T one or more of kN, and the rest operand chunks of 32 columns, four places for K and two (64 rows) or four
+// for V.  A 128-key tile is 17 chunks: nine of K (128 keys x 64 columns), eight of V (512 columns x 16 keys), four MMAs each.
 //
 // Everything is f16, not bf16: an E2M1 times an E4M3 number is exact in either, P~ has three more bits, and the conversion from
 // E2M1 gives f16.  Q is bf16: a row is multiplied by the power of two that brings its largest magnitude into [2^14, 2^15), which
@@ -19,9 +19,21 @@
 // bits and exact (nothing is left over to compensate).  P~ = 2^(a_j - n + 9): a move puts the largest P~ of a row into (2^8, 2^9], the
 // next one comes when a key would exceed 2^15, and what f16 rounds to nothing is below 2^-33 of the reference.
 //
-// Warps 0-3: Q into f16, softmax (a thread is a key and has all rows; its share of the row sums stays in registers until the unit's
-// end), rescale, epilogue.  Warps 4-11 widen K and 12-19 V, four at a time by turns; warp 20 issues the products of K, 21
-// those of V; warp 22 loads pages (bulk copies).
+// Warps: 4 (64 rows: 8, of 32 rows each group of four) for softmax, rescale and epilogue: a thread is a key and has all its rows, its share of the
+// row sums stays in registers until the unit's end.  Then 8 that widen K and 8 that widen V, in two groups of four that take chunks by
+// turns, and bring Q (all 16 of a part's first unit, K's of the others); then one each that issues K's products, V's, and the loads, which are
+// whole tiles of raw pages (bulk copies), with a note on each tile that the other warps go by.
+//
+// What bounds it: the instructions of the widening.  A tile at 64 rows takes ~4650 clk, of which the tensor pipe is busy 1750 and HBM's share is
+// ~1850; ~3300 instructions a scheduler are issued in them (16 rows: 3700, 2750), half of which are the conversions (a pair of E2M1 numbers
+// costs an operation of 2 clk), the products with the scales and, for V, the pairing of keys.  More places for operands or raw tiles, one ring for K and V in
+// place of two, a longer way of a chunk to its hand-over (all tried) change nothing or cost 3 %.  About 26 K clk a CTA (16 rows:
+// 20) are no tile's: set-up and first load 8, Q 2-6, the first tile's way through all roles, the last product and the epilogue 3-6; a further unit costs ~10.
+// 32 x 4096 keys, 128 heads: 57.4 us a call, 636 TFLOP/s (the bf16 cache: 53.0, E4M3 60.3); widening the pages into a bf16 copy in front of the bf16
+// kernels took 90.  32 x 1024-8192, 16 heads: 30.3 us, 1.6 TB/s of 4-bit pages (bf16: 37.8); 64 x 1024-8192, two tokens: 209 (bf16: 194).
+//
+// Why 64 rows at most: O^T of 128 would be all of tensor memory.  So 128 heads widen every page twice, and it is calls of few rows, or of more
+// pages than memory would hold at 16 bits, that gain.
 //
 // All waits are bounded; on expiry the kernel records kStatusTimeout and unwinds.
 #define AMLA_SELDOM __forceinline__
