@@ -7,6 +7,7 @@ import _fp4_util as F
 from paper_2509_25224_b200 import binding, paging
 from paper_2509_25224_b200.binding import AmlaError
 
+from tests.test_gpu_lengths_from_device import late  # noqa: F401
 from test_gpu_fp4 import bf16, compare, dev, expected, run, SCALE, tokens, workload
 
 pytestmark = pytest.mark.gpu
@@ -71,6 +72,37 @@ def test_lengths_that_no_table_holds_are_cut_to_it(H):
     wrong = np.array([100000, -3, 70], np.int32)
     out, lse = run(q, cache, table, wrong, 0.25)
     compare(out, lse, *expected(q, cache, table, np.array([256, 0, 70], np.int32), 0.25))
+
+
+# (the kernel for 16 rows, for 64 with the lengths on chip, with more than 512 items, with one item a row block of more than 64 rows)
+@pytest.mark.parametrize("B,Sq,H,longest", [(5, 1, 16, 900), (150, 1, 16, 200), (6, 1, 64, 900), (6, 2, 128, 900), (520, 1, 16, 100), (300, 1, 128, 150)])
+def test_lengths_written_directly_in_front_of_the_call(late, B, Sq, H, longest):  # noqa: F811
+    q, cache, table, full = workload([longest] * B, Sq, H)
+    q, cache, table = bf16(q), dev(cache), dev(table)
+    rng = np.random.default_rng(B + H)
+    one = rng.integers(0, longest + 1, B).astype(np.int32)
+    lens = [dev(x) for x in (one, np.minimum(one + 1, longest), full)]
+    garbage = dev(rng.integers(-2**31, 2**31 - 1, B, dtype=np.int64).astype(np.int32))
+    seqlens = torch.empty(B, dtype=torch.int32, device="cuda")
+    ws = torch.empty(binding.fp4_workspace_size(B, Sq, H, table.shape[1], 0), dtype=torch.uint8, device="cuda")
+
+    def decode():
+        return binding.mla_decode_fp4(q, cache, 0.25, table, seqlens, SCALE, workspace=ws)
+
+    want = []
+    for x in lens:
+        seqlens.copy_(x)
+        torch.cuda.synchronize()
+        want.append(decode())
+        torch.cuda.synchronize()
+    stream = torch.cuda.current_stream().cuda_stream
+    for delay in (0, 1000, 4000, 16000, 30000):
+        for x, (o, l) in zip(lens, want):
+            seqlens.copy_(garbage)
+            assert late(x.data_ptr(), seqlens.data_ptr(), B, delay, stream) == 0
+            out, lse = decode()
+            binding.check_status(ws)
+            assert torch.equal(out.view(torch.int16), o.view(torch.int16)) and torch.equal(lse, l)
 
 
 def test_refusals_of_tensors():
