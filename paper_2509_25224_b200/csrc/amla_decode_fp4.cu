@@ -24,11 +24,12 @@
 // turns, and bring Q (all 16 of a part's first unit, K's of the others); then one each that issues K's products, V's, and the loads, which are
 // whole tiles of raw pages (bulk copies), with a note on each tile that the other warps go by.
 //
-// What bounds it: the instructions of the widening.  A tile at 64 rows takes ~4650 clk, of which the tensor pipe is busy 1750 and HBM's share is
-// ~1850; ~3300 instructions a scheduler are issued in them (16 rows: 3700, 2750), half of which are the conversions (a pair of E2M1 numbers
-// costs an operation of 2 clk), the products with the scales and, for V, the pairing of keys.  More places for operands or raw tiles, one ring for K and V in
-// place of two, a longer way of a chunk to its hand-over (all tried) change nothing or cost 3 %.  About 26 K clk a CTA (16 rows:
-// 20) are no tile's: set-up and first load 8, Q 2-6, the first tile's way through all roles, the last product and the epilogue 3-6; a further unit costs ~10.
+// What bounds it: the widening.  A tile at 64 rows takes ~4650 clk, of which the tensor pipe is busy 1750 and HBM's share is ~1850; ~3300
+// instructions a scheduler are issued in them (16 rows: 3700, 2750), most of which convert (a pair of E2M1 numbers is one operation of 2 clk), multiply by the
+// scales (another 2) and, for V, pair keys.  What changes the waits between the roles and not that work changed nothing or cost 2-3 %: more operand
+// places, one ring for K and V, a chunk handed over later or two at a time, P~ in two halves, the next raw tile fetched as far as L2.
+// About 26 K clk a CTA (16 rows: 20) are no tile's: set-up and first load 8, Q 2-6, the first tile's way through all roles, the last product
+// and the epilogue 3-6; a further unit costs ~10.
 // 32 x 4096 keys, 128 heads: 57.4 us a call, 636 TFLOP/s (the bf16 cache: 53.0, E4M3 60.3); widening the pages into a bf16 copy in front of the bf16
 // kernels took 90.  32 x 1024-8192, 16 heads: 30.3 us, 1.6 TB/s of 4-bit pages (bf16: 37.8); 64 x 1024-8192, two tokens: 209 (bf16: 194).
 //
