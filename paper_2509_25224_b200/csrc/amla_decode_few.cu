@@ -411,7 +411,7 @@ decode_few_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_const
         if (!ok) break;
         const int row = page * kPage;
         tile.next();
-        if (tile.valid) page = __ldg(entry());               // on its way while this page waits for its slot
+        if (tile.valid) page = ldg_here(entry());               // on its way while this page waits for its slot
         load(&kv_map, row, kPieceBytes);
         if (!ok) break;
       }

@@ -803,8 +803,8 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
       int page[2] = {0, 0};                                 // the next tile's
       auto look_up = [&]() {
         const int32_t* entry = prm.block_table + static_cast<size_t>(tile.u.b) * prm.max_blocks_per_seq + tile.t;
-        page[0] = __ldg(entry);
-        if (tile.np == 2) page[1] = __ldg(entry + 1);
+        page[0] = ldg_here(entry);
+        if (tile.np == 2) page[1] = ldg_here(entry + 1);
       };
       if (tile.valid) look_up();
       while (tile.valid) {

@@ -599,7 +599,7 @@ decode_quad_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               const int t = cur.u.t0 + lt;
               const int npg = (cur.u.n_b + kPage - 1) / kPage;
               const int pg = (2 * t + half < npg) ? 2 * t + half : 2 * t;
-              page_id = __ldg(prm.block_table + static_cast<size_t>(cur.u.b) * prm.max_blocks_per_seq + pg);
+              page_id = ldg_here(prm.block_table + static_cast<size_t>(cur.u.b) * prm.max_blocks_per_seq + pg);
               k_ord = cur.ord;
               k_state = 1;
             } else {
@@ -889,7 +889,7 @@ decode_quad_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             const int t = cur.u.t0 + lt;
             const int npg = (cur.u.n_b + kPage - 1) / kPage;
             const int pg = (2 * t + (my_gp & 1) < npg) ? 2 * t + (my_gp & 1) : 2 * t;
-            page_id = __ldg(prm.block_table + static_cast<size_t>(cur.u.b) * prm.max_blocks_per_seq + pg);
+            page_id = ldg_here(prm.block_table + static_cast<size_t>(cur.u.b) * prm.max_blocks_per_seq + pg);
             have = true;
           } else {
             fin = true;

@@ -63,14 +63,15 @@ __device__ __forceinline__ uint32_t e2m1_byte(float a, float b) {
   return r;
 }
 
+// (Ordinary loads, here and of all pointers below: the kernel in front may still be writing the tokens when this one is placed.)
 // kWide: rows begin at 16 bytes, so that eight columns are one access
 template <bool kWide>
 __device__ __forceinline__ uint4 load_columns(const __nv_bfloat16* p) {
-  if (kWide) return __ldg(reinterpret_cast<const uint4*>(p));
+  if (kWide) return *reinterpret_cast<const uint4*>(p);
   uint32_t w[4];
   const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = __ldg(h + 2 * i) | (static_cast<uint32_t>(__ldg(h + 2 * i + 1)) << 16);
+  for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (static_cast<uint32_t>(h[2 * i + 1]) << 16);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <bool kWide>
@@ -87,9 +88,9 @@ __device__ __forceinline__ void store_columns(__nv_bfloat16* p, const uint32_t (
 }  // namespace
 
 template <bool kWide>
-__global__ void __launch_bounds__(kThreads) store_fp4_kernel(const __nv_bfloat16* __restrict__ kv, long long row_stride, int n_tokens, const int32_t* __restrict__ starts,
-                                                             uint8_t* __restrict__ cache, float kv_scale, const int32_t* __restrict__ block_table,
-                                                             const int32_t* __restrict__ seqlens, int B, int num_blocks, int max_blocks_per_seq) {
+__global__ void __launch_bounds__(kThreads) store_fp4_kernel(const __nv_bfloat16* kv, long long row_stride, int n_tokens, const int32_t* starts,
+                                                             uint8_t* cache, float kv_scale, const int32_t* block_table,
+                                                             const int32_t* seqlens, int B, int num_blocks, int max_blocks_per_seq) {
   __shared__ Place places[kTokens * kRounds];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
@@ -134,9 +135,9 @@ __global__ void __launch_bounds__(kThreads) store_fp4_kernel(const __nv_bfloat16
 }
 
 template <bool kWide>
-__global__ void __launch_bounds__(kThreads) load_fp4_kernel(const uint8_t* __restrict__ cache, float kv_scale, const int32_t* __restrict__ block_table,
-                                                            const int32_t* __restrict__ seqlens, const int32_t* __restrict__ starts, int B, int num_blocks,
-                                                            int max_blocks_per_seq, __nv_bfloat16* __restrict__ out, long long row_stride, int n_tokens) {
+__global__ void __launch_bounds__(kThreads) load_fp4_kernel(const uint8_t* cache, float kv_scale, const int32_t* block_table,
+                                                            const int32_t* seqlens, const int32_t* starts, int B, int num_blocks,
+                                                            int max_blocks_per_seq, __nv_bfloat16* out, long long row_stride, int n_tokens) {
   __shared__ Place places[kTokens * kRounds];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");

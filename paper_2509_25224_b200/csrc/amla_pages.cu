@@ -102,6 +102,8 @@ __device__ __forceinline__ uint32_t used_bits(const int32_t* refs, int num_block
   return used;
 }
 
+// Behind this, what the kernel in front wrote may be read.  (By ordinary loads: the kernels here are placed while it is still writing,
+// so that none of their pointers may be __restrict__ or go through __ldg, which promise that nobody else writes.)
 __device__ __forceinline__ void begin() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
@@ -109,7 +111,7 @@ __device__ __forceinline__ void begin() {
 
 // Pages of a chunk that are in use (kUsed) or free.
 template <bool kUsed>
-__global__ void __launch_bounds__(kScanThreads) count_pages_kernel(const int32_t* __restrict__ refs, int num_blocks, int* __restrict__ totals) {
+__global__ void __launch_bounds__(kScanThreads) count_pages_kernel(const int32_t* refs, int num_blocks, int* totals) {
   begin();
   uint32_t there;
   const uint32_t used = used_bits(refs, num_blocks, blockIdx.x * kChunk + threadIdx.x * kPerThread, &there);
@@ -156,8 +158,8 @@ constexpr int kRankLimit = 1 << 30;                  // a rank beyond any cache'
 
 // The free pages in order: list[rank], for the first `most` of them; head[0] = how many there are.  A block more than there are chunks
 // adds up what the requests in front of every request ask for (here, since the launch that serves them changes the lengths).
-__global__ void __launch_bounds__(kScanThreads) list_free_kernel(const int32_t* __restrict__ refs, int num_blocks, const int* __restrict__ totals, int most, int* __restrict__ head,
-                                                                 int* __restrict__ list, const Requests q, int* __restrict__ row_rank) {
+__global__ void __launch_bounds__(kScanThreads) list_free_kernel(const int32_t* refs, int num_blocks, const int* totals, int most, int* head,
+                                                                 int* list, const Requests q, int* row_rank) {
   begin();
   const int chunks = gridDim.x - 1;
   if (static_cast<int>(blockIdx.x) == chunks) {
@@ -184,7 +186,7 @@ __global__ void __launch_bounds__(kScanThreads) list_free_kernel(const int32_t* 
 
 // One block per listed row.  A row's length says whether it still holds its pages: who sets it to zero gives them up, so that a row
 // that is listed twice is freed once.
-__global__ void __launch_bounds__(kRowThreads) free_rows_kernel(int32_t* __restrict__ block_table, int32_t* __restrict__ seqlens, int32_t* __restrict__ refs, const int32_t* __restrict__ rows,
+__global__ void __launch_bounds__(kRowThreads) free_rows_kernel(int32_t* block_table, int32_t* seqlens, int32_t* refs, const int32_t* rows,
                                                                 int B, int num_blocks, int width) {
   __shared__ int length;
   begin();
@@ -203,9 +205,9 @@ __global__ void __launch_bounds__(kRowThreads) free_rows_kernel(int32_t* __restr
 
 // One row of blocks per fork, blockIdx.y of which share the copy of its last page; the first also does the books.  (Parents and
 // children are different rows, so that what is read here of a parent is not written here.)
-__global__ void __launch_bounds__(kCopyThreads) fork_rows_kernel(uint4* __restrict__ cache, int page_pieces, int32_t* __restrict__ block_table, int32_t* __restrict__ seqlens,
-                                                                 int32_t* __restrict__ refs, const Requests q, int num_blocks, const int* __restrict__ head,
-                                                                 const int* __restrict__ list, const int* __restrict__ row_rank, int32_t* __restrict__ served) {
+__global__ void __launch_bounds__(kCopyThreads) fork_rows_kernel(uint4* cache, int page_pieces, int32_t* block_table, int32_t* seqlens,
+                                                                 int32_t* refs, const Requests q, int num_blocks, const int* head,
+                                                                 const int* list, const int* row_rank, int32_t* served) {
   begin();
   const int k = blockIdx.x, width = q.width;
   const bool asked = fork_asked(q, k);
@@ -253,8 +255,8 @@ __global__ void __launch_bounds__(kCopyThreads) fork_rows_kernel(uint4* __restri
 // The whole of it by one block, for a cache of at most kChunk pages: the free pages are listed in shared memory, a thread serves a
 // row's first page and its books, the warp the others.  (64 rows, 8192 pages: 2.7 us, and 7 us of the host; as the two launches that
 // larger caches take 3.1 us, and 13.)
-__global__ void __launch_bounds__(kScanThreads) reserve_small_kernel(int32_t* __restrict__ block_table, int32_t* seqlens, int32_t* __restrict__ refs, int num_blocks, const Requests q,
-                                                                     int32_t* __restrict__ granted) {
+__global__ void __launch_bounds__(kScanThreads) reserve_small_kernel(int32_t* block_table, int32_t* seqlens, int32_t* refs, int num_blocks, const Requests q,
+                                                                     int32_t* granted) {
   __shared__ int list[kChunk];
   begin();
   const int tid = threadIdx.x, lane = tid & 31;
@@ -296,9 +298,9 @@ __global__ void __launch_bounds__(kScanThreads) reserve_small_kernel(int32_t* __
 }
 
 // One block per row.
-__global__ void __launch_bounds__(kRowThreads) reserve_rows_kernel(int32_t* __restrict__ block_table, int32_t* seqlens, int32_t* __restrict__ refs, const Requests q,
-                                                                   const int* __restrict__ head, const int* __restrict__ list, const int* __restrict__ row_rank,
-                                                                   int32_t* __restrict__ granted) {
+__global__ void __launch_bounds__(kRowThreads) reserve_rows_kernel(int32_t* block_table, int32_t* seqlens, int32_t* refs, const Requests q,
+                                                                   const int* head, const int* list, const int* row_rank,
+                                                                   int32_t* granted) {
   begin();
   const int row = blockIdx.x;
   const int now = length_of(q.seqlens, row, q.width), then = q.new_lens[row], more = reserve_asks(q, row), rank = row_rank[row];
@@ -318,8 +320,8 @@ __global__ void __launch_bounds__(kRowThreads) reserve_rows_kernel(int32_t* __re
 
 // Compaction, with `live` pages in use: the holes in front of page `live` in order (holes[i]), the pages in use behind it from the
 // last to the first (high[i]; rank[page] = i), and how many those are (head[1]).
-__global__ void __launch_bounds__(kScanThreads) list_moves_kernel(const int32_t* __restrict__ refs, int num_blocks, const int* __restrict__ totals, int* __restrict__ head, int* __restrict__ holes,
-                                                                  int* __restrict__ high, int* __restrict__ rank, int32_t* __restrict__ live_out) {
+__global__ void __launch_bounds__(kScanThreads) list_moves_kernel(const int32_t* refs, int num_blocks, const int* totals, int* head, int* holes,
+                                                                  int* high, int* rank, int32_t* live_out) {
   begin();
   uint32_t there;
   const int first = blockIdx.x * kChunk + threadIdx.x * kPerThread;
@@ -345,9 +347,9 @@ __global__ void __launch_bounds__(kScanThreads) list_moves_kernel(const int32_t*
     }
   }
 }
-__global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(uint4* __restrict__ cache, int page_pieces, int32_t* __restrict__ block_table, const int32_t* __restrict__ seqlens,
-                                                                  int32_t* __restrict__ refs, int B, int num_blocks, int width, const int* __restrict__ head, const int* __restrict__ holes,
-                                                                  const int* __restrict__ high, const int* __restrict__ rank) {
+__global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(uint4* cache, int page_pieces, int32_t* block_table, const int32_t* seqlens,
+                                                                  int32_t* refs, int B, int num_blocks, int width, const int* head, const int* holes,
+                                                                  const int* high, const int* rank) {
   begin();
   const int live = head[0], moves = head[1], segments = (page_pieces + kSegment - 1) / kSegment;
   // (the i-th hole takes the i-th page behind the line, which is the last but i of `high`)
@@ -378,7 +380,7 @@ __global__ void __launch_bounds__(kCopyThreads) move_pages_kernel(uint4* __restr
 }
 
 // Pages src[i] -> dst[i]; a pair with a page outside the cache is skipped.
-__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(uint4* __restrict__ cache, int page_pieces, int num_blocks, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(uint4* cache, int page_pieces, int num_blocks, const int32_t* src, const int32_t* dst,
                                                                   int segments) {
   begin();
   const int m = blockIdx.x / segments, seg = blockIdx.x - m * segments;
