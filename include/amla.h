@@ -195,6 +195,9 @@ int amla_mla_decode_fp4(const void* q, const void* kv_cache_fp4, float kv_scale,
  * `starts` is a device array of B + 1 that does not fall; tokens outside [starts[0], starts[B]), in front of a sequence's first
  * position, beyond the table or in a page outside [0, num_blocks) are not stored, and read back as zeros.
  *
+ * A row that amla_pages_reserve refused has not grown, so that a token stored for it would overwrite its last key, which may lie in
+ * a page that other rows hold: leave it out (a length of 0 in the call's seqlens does).
+ *
  * store: for each 16 columns, scale = e4m3(max |x| / (6 kv_scale)) and e2m1(x / (scale kv_scale)), both to nearest with ties to
  * even, both saturating.  A group that holds a NaN reads back as NaN.  Two tokens of a call must not have the same place.
  * load:  out = bf16(e2m1 * e4m3 * kv_scale), what the decode call sees.

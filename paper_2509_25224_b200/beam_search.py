@@ -64,7 +64,8 @@ def search(groups: int = 8, beams: int = 8, heads: int = 128, prompt: int = 1000
 
     def step():
         paging.pages_reserve(table, lens, refs, lens + 1, granted, scratch)
-        paging.cache_store_fp4(kv, each, cache, kv_scale, table, lens)
+        # a row that was refused has not grown: its token would land on its last key, in a page that others may hold too
+        paging.cache_store_fp4(kv, each, cache, kv_scale, table, lens * granted)
         attend()
         score.add_(lse.mean((1, 2)).view(groups, beams))
         order = score.argsort(1)
@@ -75,20 +76,23 @@ def search(groups: int = 8, beams: int = 8, heads: int = 128, prompt: int = 1000
         paging.pages_fork(cache, table, lens, refs, best, worst, served, scratch)
         failed.add_((granted == 0).sum() + (served == 0).sum())
 
-    history = torch.empty((rows, longest, 576), dtype=torch.bfloat16, device=dev)
-    history[:, :prompt] = tokens.repeat_interleave(beams, 0)
+    # what every row should hold: its tokens from the left, zeros behind them (a row that found no page has fewer than the others)
+    history, row, had = torch.zeros((rows, longest, 576), dtype=torch.bfloat16, device=dev), torch.arange(rows, device=dev), torch.empty_like(lens)
+    history[:, :prompt] = tokens.repeat_interleave(beams, 0) * (lens == prompt)[:, None, None]
 
-    def inputs(i):
+    def inputs():
         q.normal_(generator=gen)
         kv.normal_(generator=gen)
-        history[:, prompt + i] = kv
+        had.copy_(lens)
 
     def remember():
-        history[worst.long()] = history[best.long()]
+        at = row, had.long()
+        history[at] = torch.where(granted[:, None] > 0, kv, history[at])
+        history[worst.long()] = history[best.long()] * (served > 0)[:, None, None]
 
     graph, times = None, []
     for i in range(steps):
-        inputs(i)
+        inputs()
         if i == 1:
             graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(graph):
@@ -111,10 +115,13 @@ def search(groups: int = 8, beams: int = 8, heads: int = 128, prompt: int = 1000
     attend()
     read = torch.empty((rows * longest, 576), dtype=torch.bfloat16, device=dev)
     paging.cache_load_fp4(cache, kv_scale, table, lens, torch.arange(0, (rows + 1) * longest, longest, **int32), read)
+    # (the last tokens of a row end at the right)
+    at = torch.arange(longest, device=dev) + (longest - lens.long())[:, None]
+    read = read.view(rows, longest, 576)[row[:, None], at.clamp(max=longest - 1)] * (at < longest)[..., None]
     binding.check_status(work)
     spent = sorted(a.elapsed_time(b) * 1e3 for a, b in times[2:])
     return dict(cache=cache, kv_scale=kv_scale, scale=scale, q=q, out=out, lse=lse, before=before, table=table, lens=lens, refs=refs, history=history,
-                read=read.view(rows, longest, 576), live=int(live), failed=int(failed), step_us=spent[len(spent) // 2] if spent else None, width=width)
+                read=read, live=int(live), failed=int(failed), step_us=spent[len(spent) // 2] if spent else None, width=width)
 
 
 def faults(r) -> list[str]:

@@ -43,3 +43,14 @@ def test_a_cache_that_is_too_small_is_reported():
     assert r["failed"] > 0 and "found no page" in beam_search.faults(r)[0]
     with pytest.raises((AmlaError, ValueError, RuntimeError)):
         beam_search.search(1, 4, 16, 60, 8, num_blocks=0)
+
+
+# (a shared full page with two pages left for four rows; a prompt whose last page is not full; two groups over many pages; a group without a prompt)
+@pytest.mark.parametrize("groups,beams,prompt,steps,num_blocks", [(1, 4, 64, 8, 3), (1, 4, 60, 8, 3), (2, 4, 128, 70, 9), (2, 3, 63, 5, 1)])
+def test_rows_that_find_no_page_leave_the_others_alone(groups, beams, prompt, steps, num_blocks):
+    r = beam_search.search(groups, beams, 16, prompt, steps, kv_scale=0.25, num_blocks=num_blocks)
+    assert r["failed"] > 0
+    # every row, refused ones too, still reads back as the tokens that it was granted
+    assert beam_search.faults(r) == ["%d requests found no page" % r["failed"], "a row has the wrong length"]
+    lens = r["lens"].cpu().numpy()
+    assert lens.max() > 0 and (r["read"].abs().sum(-1) > 0).sum(1).tolist() == lens.tolist()
