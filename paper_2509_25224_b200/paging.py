@@ -193,7 +193,8 @@ def pages_fork(cache, block_table, seqlens, refs, parents, children, served=None
 
 
 def pages_reserve(block_table, seqlens, refs, new_lens, granted=None, workspace=None):
-    """Rows grow to new_lens [B], with free pages where they need them.  Returns granted int32 [B]: 0 where the row stays as it was."""
+    """Rows grow to new_lens [B], with free pages where they need them.  Returns granted int32 [B]: 0 where the row stays as it was
+    (which takes no page from the rows behind it)."""
     L = _ready()
     on, B, width, blocks = _books(block_table, seqlens, refs)
     _int32(new_lens, on, "new_lens")
