@@ -175,9 +175,10 @@ __host__ __device__ inline int merge_groups(const DecodeParams& prm) { return pr
 // more mantissa bits), each 32-column chunk of a row scaled by a power of two so that its largest magnitude lies in
 // [1, 2): the chunk's scale byte is the biased FP32 exponent of that magnitude, the stored halves are value *
 // 2^(127 - byte), and value = half * 2^(byte - 127) exactly (byte 0: a chunk of zeros).  Half the bytes of FP32
-// partials, whatever the range of V.  (The kernel for few rows leaves FP32 rows [2 * P * 32][512]: its partials are small,
+// partials, whatever the range of V.  (The kernel for few rows of a bf16 cache leaves FP32 rows [2 * P * 32][512]: its partials are small,
 // and a thread of it holds a column, so that a chunk's largest magnitude would be a reduction over the warp for every row:
-// 10 K of an epilogue's 13 K clk.)
+// 10 K of an epilogue's 13 K clk.  The kernel for a 4-bit cache, whose values have a known largest, leaves halves against one power of two
+// whatever its rows, and looks for a row's own, over 128 columns, only where that one would lose bits.)
 // ---------------------------------------------------------------------------------------------
 __host__ __device__ inline size_t partial_rows(const DecodeParams& prm) { return static_cast<size_t>(2) * prm.P * prm.item_rows; }
 __device__ __forceinline__ uint16_t* partial_halves(const DecodeParams& prm) { return reinterpret_cast<uint16_t*>(prm.part_o); }
