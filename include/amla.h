@@ -229,7 +229,8 @@ int amla_cache_load_fp4(const void* kv_cache_fp4, float kv_scale, const int32_t*
  *          left (the child is then empty) or an index is outside [0, B) or child == parent (nothing happens).
  * reserve  rows grow to new_lens[b] (a shorter one leaves the row as it is), with free pages for the positions that need them.  granted[b]
  *          (or NULL): 1, or 0 where the table or the pages left by the rows before it do not suffice; the row is then as it was, and
- *          takes no page: a row behind it that asks for fewer may be granted.  new_lens must not be seqlens itself.
+ *          takes no page: a row behind it that asks for fewer may be granted.  new_lens and granted must not overlap
+ *          seqlens, nor each other (but they may be the same).
  * compact  with L pages in use, the i-th page in use at or behind page L moves to the i-th free page in front of it: contents,
  *          refs and the rows' entries.  Pages L .. are free afterwards; *live (device, or NULL) = L.
  */

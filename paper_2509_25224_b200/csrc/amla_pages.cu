@@ -467,6 +467,10 @@ int check_workspace(const void* workspace, size_t bytes, int num_blocks, int row
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & (kAlign - 1))) return AMLA_ERR_INVALID_ARG;
   return bytes < scratch_bytes(num_blocks, rows) ? AMLA_ERR_WORKSPACE : AMLA_OK;
 }
+bool overlap(const int32_t* a, const int32_t* b, int n) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), bytes = sizeof(int32_t) * static_cast<uintptr_t>(n);
+  return a != nullptr && x < y + bytes && y < x + bytes;
+}
 bool odd_int(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) != 0; }
 
 cudaError_t list_free(const int32_t* refs, int num_blocks, long long most, const Requests& q, const Scratch& s, cudaStream_t stream) {
@@ -533,9 +537,12 @@ extern "C" int amla_pages_reserve(int32_t* block_table, int32_t* seqlens, int32_
                                   void* workspace, size_t workspace_bytes, void* cuda_stream) {
   int rc = check_books(block_table, seqlens, refs, B, num_blocks, max_blocks_per_seq);
   if (rc != AMLA_OK) return rc;
-  if (!new_lens || odd_int(new_lens) || odd_int(granted) || new_lens == seqlens) return AMLA_ERR_INVALID_ARG;
+  if (!new_lens || odd_int(new_lens) || odd_int(granted)) return AMLA_ERR_INVALID_ARG;
+  // (a row is served by one thread, or block: what it writes must not be what another one still reads)
+  if (overlap(new_lens, seqlens, B)) return AMLA_ERR_INVALID_ARG;
   rc = check_workspace(workspace, workspace_bytes, num_blocks, B);
   if (rc != AMLA_OK) return rc;
+  if (overlap(granted, seqlens, B) || (granted != new_lens && overlap(granted, new_lens, B))) return AMLA_ERR_INVALID_ARG;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const Requests q{seqlens, nullptr, nullptr, new_lens, B, B, max_blocks_per_seq};
   if (chunks_of(num_blocks) == 1) return done(launch(reserve_small_kernel, dim3(1), kScanThreads, stream, block_table, seqlens, refs, num_blocks, q, granted));
