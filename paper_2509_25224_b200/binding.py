@@ -44,6 +44,7 @@ EXPORTS = [
 
 _lib = None
 _PAGE_SHAPE = (64, 576)
+_WORKSPACE = "workspace must be a contiguous tensor on the inputs' device"
 _FP4_PAGE_SHAPE = (64 * (576 // 2 + 576 // 16),)      # 64 rows of E2M1 pairs, then 64 rows of E4M3 scales
 
 
@@ -204,6 +205,8 @@ def mla_decode_fp8(q, kv_cache_e4m3, kv_scale: float, block_table, seqlens, soft
         lse = torch.empty((B, Sq, H), dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = torch.empty(fp8_workspace_size(B, Sq, H, block_table.shape[1], dev.index or 0), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(_WORKSPACE)
     if _lib is None:
         lib()
     _on_device(dev, _lib.amla_mla_decode_fp8,
@@ -250,6 +253,8 @@ def mla_decode_fp4(q, kv_cache_fp4, kv_scale: float, block_table, seqlens, softm
         raise ValueError("lse must be a contiguous float32 [B,Sq,H] on the inputs' device")
     if workspace is None:
         workspace = torch.empty(fp4_workspace_size(B, Sq, H, block_table.shape[1], dev.index or 0), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(_WORKSPACE)
     _on_device(dev, _lib.amla_mla_decode_fp4,
                (q.data_ptr(), kv_cache_fp4.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), float(softmax_scale), B, Sq, H,
                 kv_cache_fp4.shape[0], block_table.shape[1], out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size()),
@@ -375,6 +380,8 @@ def mla_decode(q, kv_cache, block_table, seqlens, softmax_scale: float, out=None
     if workspace is None:
         workspace = torch.empty(workspace_size(B, Sq, H, block_table.shape[1], dev.index or 0),
                                 dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(_WORKSPACE)
     args = (q.data_ptr(), kv_cache.data_ptr(), block_table.data_ptr(), seqlens.data_ptr(), float(softmax_scale), B, Sq, H, kv_cache.shape[0],
             block_table.shape[1], out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.numel())
     if flags is None:
