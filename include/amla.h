@@ -261,6 +261,13 @@ int amla_check_status(const void* workspace, void* cuda_stream);
 int amla_wait_selftest(void* workspace, unsigned long long limit_ns, void* cuda_stream);
 
 /*
+ * The same for the waits of the kernel for a 4-bit cache, which count tries (1 .. 4096 here).  `report` (device, int32 [5]): the tries left behind a wait
+ * on a barrier that nothing arrives on, behind a second one with none left, and behind one on a barrier that is complete; the nanoseconds that the
+ * first and the second took.
+ */
+int amla_wait_tries_selftest(void* workspace, int tries, int* report, void* cuda_stream);
+
+/*
  * Debug aid, host only: checks HOST copies of the paging inputs before a decode call.  Every seqlens[b] must lie
  * in [0, 64 * max_blocks_per_seq] and every block_table entry that the sequence uses (the first
  * ceil(seqlens[b] / 64) of row b) in [0, num_blocks).  Returns AMLA_OK, or AMLA_ERR_INVALID_ARG with the

@@ -36,7 +36,7 @@ DEFAULT_FLAGS = RESCALE_ALG2 | lazy(DEFAULT_TAU)   # what amla_mla_decode (witho
 EXPORTS = [
     "amla_status_string", "amla_mla_decode_workspace_size", "amla_mla_decode", "amla_mla_decode_ex",
     "amla_check_status", "amla_last_launch_count", "amla_plan_host", "amla_profile_enable",
-    "amla_profile_last_ms", "amla_mla_decode_static", "amla_static_check_status", "amla_wait_selftest",
+    "amla_profile_last_ms", "amla_mla_decode_static", "amla_static_check_status", "amla_wait_selftest", "amla_wait_tries_selftest",
     "amla_last_item_rows", "amla_validate_paging_host", "amla_mla_decode_fp8", "amla_mla_decode_fp8_workspace_size",
     "amla_mla_decode_fp4", "amla_mla_decode_fp4_workspace_size", "amla_cache_store_fp4", "amla_cache_load_fp4",
     "amla_pages_workspace_size", "amla_pages_copy", "amla_pages_free", "amla_pages_fork", "amla_pages_reserve", "amla_pages_compact",
@@ -103,6 +103,8 @@ def lib() -> ctypes.CDLL:
         L.amla_static_check_status.restype = i32
         L.amla_wait_selftest.argtypes = [vp, ctypes.c_ulonglong, vp]
         L.amla_wait_selftest.restype = i32
+        L.amla_wait_tries_selftest.argtypes = [vp, i32, vp, vp]
+        L.amla_wait_tries_selftest.restype = i32
         L.amla_validate_paging_host.argtypes = [vp, vp, i32, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32)]
         L.amla_validate_paging_host.restype = i32
         L.amla_check_status.argtypes = [vp, vp]
@@ -275,6 +277,13 @@ def wait_selftest(workspace, limit_ns: int = 1_000_000, stream: int = 0) -> None
     rc = lib().amla_wait_selftest(workspace.data_ptr(), int(limit_ns), stream)
     if rc != AMLA_OK:
         raise AmlaError(rc, "amla_wait_selftest")
+
+
+def wait_tries_selftest(workspace, report, tries: int = 256, stream: int = 0) -> None:
+    """The same for waits that count tries; `report` int32 [5] is what amla.h says."""
+    rc = lib().amla_wait_tries_selftest(workspace.data_ptr(), int(tries), report.data_ptr(), stream)
+    if rc != AMLA_OK:
+        raise AmlaError(rc, "amla_wait_tries_selftest")
 
 
 def validate_paging_host(block_table, seqlens, num_blocks: int):

@@ -18,6 +18,7 @@ cudaError_t launch_decode_pair(const DecodeParams& prm, cudaStream_t stream, int
 cudaError_t launch_decode_few(const DecodeParams& prm, cudaStream_t stream, int* unsupported);
 cudaError_t launch_decode_quad(const DecodeParams& prm, cudaStream_t stream, int* unsupported);
 cudaError_t launch_wait_selftest(int* status, unsigned long long limit_ns, cudaStream_t stream);
+cudaError_t launch_tries_selftest(int* status, int tries, int* report, cudaStream_t stream);
 cudaError_t launch_widen_pages(const uint8_t* kv8, const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks,
                                int max_blocks_per_seq, __nv_bfloat16* scratch, int32_t* table_out, cudaStream_t stream);
 cudaError_t launch_decode_fp4(const DecodeParams& prm, cudaStream_t stream);
@@ -452,6 +453,16 @@ extern "C" int amla_wait_selftest(void* workspace, unsigned long long limit_ns, 
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 3)) return AMLA_ERR_INVALID_ARG;
   if (limit_ns == 0 || limit_ns > 100000000ull) return AMLA_ERR_INVALID_ARG;      // at most 0.1 s
   if (launch_wait_selftest(static_cast<int*>(workspace), limit_ns, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) {
+    cudaGetLastError();
+    return AMLA_ERR_CUDA;
+  }
+  return AMLA_OK;
+}
+
+extern "C" int amla_wait_tries_selftest(void* workspace, int tries, int* report, void* cuda_stream) {
+  if (!workspace || !report || ((reinterpret_cast<uintptr_t>(workspace) | reinterpret_cast<uintptr_t>(report)) & 3)) return AMLA_ERR_INVALID_ARG;
+  if (tries < 1 || tries > 4096) return AMLA_ERR_INVALID_ARG;
+  if (launch_tries_selftest(static_cast<int*>(workspace), tries, report, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) {
     cudaGetLastError();
     return AMLA_ERR_CUDA;
   }
