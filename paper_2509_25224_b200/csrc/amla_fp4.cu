@@ -51,10 +51,10 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 // x / step, inv = fl(1 / step) (0 for a group of zeros).  What is beyond E2M1's 6 by far saturates whatever its last bits are (and the
-// remainder of an infinity is a NaN).
+// remainder of an infinity is a NaN).  The sign is x's, of a zero too (the remainder of -0 is +0).
 __device__ __forceinline__ float quotient(float x, float step, float inv) {
   const float y = x * inv;
-  return fabsf(y) < 16.f ? fmaf(fmaf(-y, step, x), inv, y) : y;
+  return copysignf(fabsf(y) < 16.f ? fmaf(fmaf(-y, step, x), inv, y) : y, x);
 }
 // low half: a, high half: b
 __device__ __forceinline__ uint32_t e2m1_byte(float a, float b) {
