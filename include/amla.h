@@ -81,7 +81,8 @@ int amla_mla_decode_workspace_size(int B, int Sq, int H, int max_blocks_per_seq,
  * Key j of sequence b is row (j % 64) of page block_table[b][j / 64] of kv_cache.  Query token t sees
  * key j iff 0 <= j < seqlens[b] and j <= seqlens[b] - Sq + t (the Sq query tokens are the last Sq
  * positions; each sees itself and everything before).  A row with no visible key gets out = 0,
- * lse = -inf.
+ * lse = -inf.  A row whose q holds a NaN or an infinity has no sum that is a number: it gets lse = -inf, and NaN or (where its sequence is
+ * split) zeros in out; no other row notices.
  *
  *   q            device, bf16 [B, Sq, H, 576], contiguous, 16-byte aligned
  *   kv_cache     device, bf16 [num_blocks, 64, 576], contiguous, 16-byte aligned.  Rows of a used page
@@ -180,7 +181,7 @@ int amla_mla_decode_fp8(const void* q, const void* kv_cache_e4m3, float kv_scale
  *   workspace      at least amla_mla_decode_fp4_workspace_size() bytes, 256-byte aligned
  *
  * A call reads 324 bytes a key (bf16: 1152).  Rows of a used page beyond the sequence length may hold anything.  A scale that is
- * a NaN makes the rows that see the key NaN.  A block-table entry outside [0, num_blocks) of a used page reads
+ * a NaN makes the rows that see the key NaN, out and lse; a row whose q holds a NaN or an infinity is NaN too.  A block-table entry outside [0, num_blocks) of a used page reads
  * as a page of zeros.  Everything else (visibility rule, outputs, shapes, errors) is as for amla_mla_decode; amla_check_status reads the status.
  */
 int amla_mla_decode_fp4_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int device, size_t* bytes_out);
