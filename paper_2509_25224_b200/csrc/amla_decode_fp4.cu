@@ -13,7 +13,7 @@
 //
 // Everything is f16, not bf16: an E2M1 times an E4M3 number is exact in either, P~ has three more bits, and the conversion from
 // E2M1 gives f16.  Q is bf16: a row is multiplied by the power of two that brings its largest magnitude into [2^14, 2^15), which
-// leaves every element within 2^-32 of the row's largest exact, and smaller ones off by at most 2^-25 in units of which the largest has 2^14.
+// leaves every element within 2^-31 of the row's largest exact, and smaller ones off by at most 2^-25 in units of which the largest has 2^14.
 //
 // The reference of the online softmax is an integer number of octaves n, so that a rescale of O and l is an add to the exponent
 // bits and exact (nothing is left over to compensate).  P~ = 2^(a_j - n + 9): a move puts the largest P~ of a row into (2^8, 2^9], the
@@ -29,12 +29,15 @@
 // scales (another 2) and, for V, pair keys.  What changes the waits between the roles and not that work changed nothing or cost 2-3 %: more operand
 // places, one ring for K and V, a chunk handed over later or two at a time, P~ in two halves, the next raw tile fetched as far as L2.
 // About 26 K clk a CTA (16 rows: 20) are no tile's: set-up and first load 8, Q 2-6, the first tile's way through all roles, the last product
-// and the epilogue 3-6; a further unit costs ~10.
-// 32 x 4096 keys, 128 heads: 57.4 us a call, 636 TFLOP/s (the bf16 cache: 53.0, E4M3 60.3); widening the pages into a bf16 copy in front of the bf16
-// kernels took 90.  32 x 1024-8192, 16 heads: 30.3 us, 1.6 TB/s of 4-bit pages (bf16: 37.8); 64 x 1024-8192, two tokens: 209 (bf16: 194).
+// and the epilogue 3-6; a further unit costs ~10, since there is one buffer of Q and one O^T, and the warps that widen K bring Q.  With 16 rows that is 20 of 50
+// K clk, as much as the widening in the others.
+// 32 x 4096 keys, 128 heads: 57.0 us a call, 641 TFLOP/s (the bf16 cache: 50.1); 64 x 1024-8192, two tokens: 205 (bf16: 168); 32 x 1024-8192, 16 heads: 30.3,
+// 1.6 TB/s of 4-bit pages (bf16: 36.3), 32 heads: 33.1 (41.4), 64: 43.8 (54.0).  (In turn on one GPU, a second each.)  Widening the pages into a bf16 copy in
+// front of the bf16 kernels took 90 for the first.
 //
-// Why 64 rows at most: O^T of 128 would be all of tensor memory.  So 128 heads widen every page twice, and it is calls of few rows, or of more
-// pages than memory would hold at 16 bits, that gain.
+// Why 64 rows at most: O^T of 128 would be all of a CTA's tensor memory.  So 128 heads widen every page twice, two tokens of them four times, and are slower than
+// from a bf16 cache; calls of few rows gain, and those of more pages than memory would hold at 16 bits.  (A pair MMA, M = 256, takes each half of A from
+// its own CTA's tensor memory, so that a pair could widen half a page each for 128 rows: not built.)
 //
 // All waits are bounded; on expiry the kernel records kStatusTimeout and unwinds.
 #define AMLA_SELDOM __forceinline__

@@ -7,9 +7,9 @@
 // A group that holds a NaN gets the scale NaN and reads back as NaN; an infinity saturates (2688 kv_scale).
 //
 // Both are streams: 1152 bytes of bf16 and 324 of cache a token.  A thread does eight columns (16 bytes of bf16, one 32-bit
-// word of codes), 72 threads a token, so that every access of a warp is to whole neighbouring sectors.  A step's 96 tokens take 2.7 us
-// (a launch, and a search for the sequence, its length and its page, each read after the other), and 7 of the host; the host
-// still bounds both calls where 4 x 2048 tokens are stored and 23 k loaded: 14.8 us together, 3.1 TB/s.
+// word of codes), 72 threads a token, so that every access of a warp is to whole neighbouring sectors.  A step's 96 tokens take 3.0 us, to load them 2.8
+// (a launch, and a search for the sequence, its length and its page, each read after the other), and 7 of the host.  4 x 2048 tokens are stored in 5.7 us and
+// 23 k loaded in 10.0, from memory (2.1 and 3.4 TB/s; 4.4 and 7.3 from L2), which is as long as the host takes for the two calls.
 #include <cuda_bf16.h>
 
 #include "../../include/amla.h"

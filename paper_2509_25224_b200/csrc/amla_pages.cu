@@ -8,7 +8,8 @@
 //
 // What bounds them: the books are some kilobytes, so that free, fork, reserve and a compaction that finds nothing to move cost their launches
 // and a few dependent reads (1.3, 3.6, 2.8 and 8.2 us in a graph, 64 rows of 128 entries and 8192 pages); copies are bound by the
-// memory, which takes 16 bytes a thread four deep at full occupancy: 8 192 pages of 20 736 bytes move at the rate of a plain copy.
+// memory, which takes 16 bytes a thread four deep at full occupancy: a list of 5000 pages of 36 864 bytes moves at 98 % of the rate of a plain copy, a
+// compaction of 2900 of 73 728 at 85 % with its launches.
 #include <algorithm>
 
 #include "../../include/amla.h"
@@ -28,8 +29,8 @@ constexpr int kSegment = kCopyThreads * kCopyUnroll; // 16-byte pieces that a bl
 // Blocks that move pages.  How many there are to move is only known on the device, so that a block takes every kMoveBlocks-th piece
 // of the work.  9 948 moves of 20 736 bytes (412 MB), with the launches in front and the events' own 5 us: 87 us with the eight
 // blocks that an SM holds (the second segment of a page is short, and a block has always the one kind or the other), 79 with four
-// times as many, which are dealt out as others end, 97 with one for every piece that there might be.  (A compaction of 8192 pages that
-// finds nothing to move: 4.2, 8.2.)
+// times as many, which are dealt out as others end, 97 with one for every piece that there might be.  (2900 moves of 73 728, 428 MB, with the call and a copy of
+// the books and without events: 82.6, 78.4.  A compaction of 8192 pages that finds nothing to move: 4.2, 8.2.)
 constexpr int kMoveBlocks = 148 * 32;
 constexpr size_t kAlign = 256;
 
