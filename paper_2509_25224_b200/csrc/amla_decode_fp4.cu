@@ -106,7 +106,7 @@ struct Shape {
   static constexpr uint32_t kOCol = 0, kSCol = 4 * kN, kKCol = 512 - 32 * (kKBufs + kVBufs), kVCol = 512 - 32 * kVBufs;
   enum { X_FULL = 0, X_EMPTY = X_FULL + kSlots, X_KFULL = X_EMPTY + kSlots, X_KEMPTY = X_KFULL + kKBufs, X_VFULL = X_KEMPTY + kKBufs, X_VEMPTY = X_VFULL + kVBufs, X_QREADY = X_VEMPTY + kVBufs,
          X_SFULL = X_QREADY + kUnitsAhead, X_SEMPTY = X_SFULL + kSBufs, X_PREADY = X_SEMPTY + kSBufs, X_PVDONE, X_MOVES, X_MAX = X_MOVES + kGroups, X_SUMS = X_MAX + kGroups,
-         X_START = X_SUMS + kGroups, X_NUM };
+         X_START = X_SUMS + kGroups, X_QKDRAIN, X_PVDRAIN, X_NUM };
   static_assert(X_NUM * 8 + 8 <= kBarBytes, "barrier area too small");
   static_assert(kBytes <= 232448, "exceeds the shared memory a block can opt in to");
   static_assert(kOffP % 1024 == 0 && kOffRaw % 1024 == 0 && kTileBytes % 16 == 0 && kOffBars % 8 == 0, "alignment");
@@ -211,6 +211,8 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
     mbar_init(bar(C::X_PREADY), kSoftmaxWarps);
     mbar_init(bar(C::X_PVDONE), 1);
     mbar_init(bar(C::X_START), 1);
+    mbar_init(bar(C::X_QKDRAIN), 1);
+    mbar_init(bar(C::X_PVDRAIN), 1);
     for (int i = 0; i < C::kGroups; ++i) { mbar_init(bar(C::X_MOVES + i), 4); mbar_init(bar(C::X_MAX + i), 4); mbar_init(bar(C::X_SUMS + i), 4); }
     fence_mbar_init();
   }
@@ -235,6 +237,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
   constexpr uint32_t tbase = 0;
   if (ld_shared_b32(tmem_slot) != 0) {
     if (tid == 0) report_timeout(prm.status);
+    if (wid == C::kQkWarp) tmem_dealloc(ld_shared_b32(tmem_slot), 512);
     return;
   }
 
@@ -744,6 +747,13 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
     constexpr uint32_t dhi = smem_desc_hi_sw128(1024);
+    // A wait that runs out is noticed at the end of its tile, so that products have been issued behind it: they are waited for, before the tensor memory
+    // that they read and write is given back.
+    auto give_up = [&](uint32_t drained) {
+      report_timeout(prm.status);
+      mma_commit(drained);
+      mbar_wait_inline(drained, 0);
+    };
     if (wid == C::kQkWarp) {
       // ======================================================== S^T = K Q^T
       // (Constants wherever they can be: an accumulate flag out of a register alone costs as much issue as an MMA.)
@@ -780,7 +790,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           left = kWaitTries;
           more = ok && !(note & kLastTile);
         }
-        if (!ok) report_timeout(prm.status);
+        if (!ok) give_up(bar(C::X_QKDRAIN));
       }
       __syncwarp();
     } else if (wid == C::kPvWarp) {
@@ -818,7 +828,7 @@ __global__ void __launch_bounds__(Shape<kN>::kThreads, 1) decode_fp4_kernel(cons
           left = kWaitTries;
           more = ok && !(note & kLastTile);
         }
-        if (!ok) report_timeout(prm.status);
+        if (!ok) give_up(bar(C::X_PVDRAIN));
       }
       __syncwarp();
     } else if (wid == kLoadWarp) {
