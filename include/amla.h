@@ -247,6 +247,70 @@ int amla_pages_reserve(int32_t* block_table, int32_t* seqlens, int32_t* refs, co
 int amla_pages_compact(void* cache, long long page_bytes, int32_t* block_table, const int32_t* seqlens, int32_t* refs, int B,
                        int num_blocks, int max_blocks_per_seq, int32_t* live, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * New tokens into a cache of any format, with what a model does to them directly in front of it (no counterpart in the paper).
+ *   format       AMLA_CACHE_BF16 (bf16 [num_blocks, 64, 576]), AMLA_CACHE_E4M3 (uint8 [num_blocks, 64, 576], value = e4m3 * kv_scale) or
+ *                AMLA_CACHE_FP4 (as for amla_cache_store_fp4); kv_scale 2^-100 .. 2^100, not used by bf16
+ *   kv, starts   the batch's tokens, rows of 576 bf16 `row_stride` elements apart, and which of them are whose: as for amla_cache_store_fp4, and so
+ *                are the tokens that are not stored.  Two tokens of a call must not have the same place.
+ *   cos_sin      fp32 [n_positions, 64], 16-byte aligned: for each position the cosines of its 32 angles, then their sines
+ *   positions    int32 [n_tokens], or NULL: the position of a token is its place in its sequence.  A token whose position is outside
+ *                [0, n_positions) is not stored, and its queries are left as they are.
+ *   norm_weight  [512], bf16 or fp32 (weight_is_f32), or NULL: the latent columns are stored as they come (then eps is not used)
+ *   interleaved  which columns make a pair: 2 i and 2 i + 1, or (0) i and i + 32
+ *   q_pe, q, H   H heads of queries for each token (0: none; at most 1024): the 64 columns at q_pe + token * q_pe_token_stride + head * q_pe_head_stride are
+ *                rotated by the token's angles into columns 512 .. 575 of the row at q + token * q_token_stride + head * q_head_stride; the others
+ *                are not touched.  Strides in elements; rows of q must not overlap one another, q_pe may be those columns of q themselves.
+ * c' = c * rsqrt(mean(c^2) + eps) * norm_weight over the 512 latent columns; (x, y) -> (x cos - y sin, y cos + x sin) for the 32 pairs of the
+ * others, both in FP32 and rounded once, to nearest with ties to even, to what the cache or q holds (E4M3 and E2M1 saturate).  A NaN stays one (4 bits: with its group).
+ * Rows, weights and strides that allow 16-byte accesses throughout get them.
+ */
+enum { AMLA_CACHE_BF16 = 0, AMLA_CACHE_E4M3 = 1, AMLA_CACHE_FP4 = 2 };
+int amla_cache_append(int format, const void* kv, long long row_stride, int n_tokens, const int32_t* starts, void* kv_cache, float kv_scale,
+                      const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks, int max_blocks_per_seq, const float* cos_sin,
+                      int n_positions, const int32_t* positions, const void* norm_weight, int weight_is_f32, float eps, int interleaved,
+                      const void* q_pe, long long q_pe_token_stride, long long q_pe_head_stride, void* q, long long q_token_stride,
+                      long long q_head_stride, int H, void* cuda_stream);
+
+/*
+ * Summaries of pages: for every page whose last key is one of the call's tokens (starts as above, n_tokens of them at most), means[page] = the mean
+ * of its 64 keys as the decode calls see them, summed in FP32.  means: bf16 [num_blocks, 576], 16-byte aligned; the other pages' are left as they were.  A
+ * page that is shared, or copied when it is not full (amla_pages_fork), keeps or gets its summary this way; pages that are moved
+ * (amla_pages_compact, amla_pages_copy) do not take theirs along: call this with all tokens of the sequences.
+ */
+int amla_page_means(int format, const void* kv_cache, float kv_scale, const int32_t* block_table, const int32_t* seqlens, const int32_t* starts,
+                    int n_tokens, int B, int num_blocks, int max_blocks_per_seq, void* means, void* cuda_stream);
+
+/*
+ * Attention to a part of a long context (no counterpart in the paper).  Query token t of sequence b sees n = max(0, seqlens[b] - Sq + t + 1) keys
+ * in ceil(n / 64) pages.
+ *
+ * scores: scores[b,t,p] = sum_h softmax_p(softmax_scale * q[b,t,h,:] . means[page p of sequence b]) over the pages p in front of the one that holds
+ *         the query token's own position, which are full; 0 elsewhere.  It is the heads' attention that a page would have, were all of its keys
+ *         their mean.  scores: fp32 [B, Sq, max_blocks_per_seq], 16-byte aligned.  A table entry outside [0, num_blocks) counts as a mean of zeros.  A row of q that
+ *         holds a NaN or an infinity makes its token's scores NaN.
+ * select: of the pages that a token sees, the first `sink`, the last `recent` (at least 1) and, of the others, those with the largest scores,
+ *         `keep` in all (sink + recent <= keep); where scores are equal the lower position comes first, and a NaN counts as -infinity.
+ *         Scores of other pages are not read.  For row r = b * Sq + t: table[r] (int32 [B * Sq, keep]) has the pages' entries of the block
+ *         table in order of position, lens[r] (int32 [B * Sq]) the number of keys in them (all but the last page are full), chosen[r] (int32 [B * Sq, keep], or NULL) their
+ *         positions in block_table[b]; -1 beyond.  table and lens are a block table and lengths for any of the decode
+ *         calls on B * Sq sequences of one query token each (q [B, Sq, H, 576] as it lies).
+ * decode: all of it: scores, selection, attention.  lse is that of the keys attended to.  Where max_blocks_per_seq <= keep no page is left out, means is not
+ *         read (and may be NULL), and the result is that of the plain call.
+ * workspace: 256-byte aligned, at least as many bytes as the size function says; 1 <= Sq <= 8, 1 <= H <= 128, B * max_blocks_per_seq <= 2^28.  The status is read with
+ * amla_check_status for scores and amla_sparse_check_status for decode.
+ */
+int amla_page_scores_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int device, size_t* bytes_out);
+int amla_page_scores(const void* q, const void* means, const int32_t* block_table, const int32_t* seqlens, float softmax_scale, int B, int Sq, int H,
+                     int num_blocks, int max_blocks_per_seq, float* scores, void* workspace, size_t workspace_bytes, void* cuda_stream);
+int amla_pages_select(const float* scores, const int32_t* block_table, const int32_t* seqlens, int B, int Sq, int max_blocks_per_seq, int keep, int sink,
+                      int recent, int32_t* table, int32_t* lens, int32_t* chosen, void* cuda_stream);
+int amla_mla_decode_sparse_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int keep, int device, size_t* bytes_out);
+int amla_mla_decode_sparse(int format, const void* q, const void* kv_cache, float kv_scale, const void* means, const int32_t* block_table, const int32_t* seqlens,
+                           float softmax_scale, int B, int Sq, int H, int num_blocks, int max_blocks_per_seq, int keep, int sink, int recent,
+                           void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+int amla_sparse_check_status(const void* workspace, void* cuda_stream);
+
 /* Synchronises `cuda_stream` and reads the status word the kernels keep at the start of the
  * workspace: AMLA_OK, or AMLA_ERR_DEVICE_TIMEOUT if a bounded wait inside a kernel expired (the
  * kernel then returned early and the outputs are undefined).  Optional. */

@@ -40,6 +40,8 @@ EXPORTS = [
     "amla_last_item_rows", "amla_validate_paging_host", "amla_mla_decode_fp8", "amla_mla_decode_fp8_workspace_size",
     "amla_mla_decode_fp4", "amla_mla_decode_fp4_workspace_size", "amla_cache_store_fp4", "amla_cache_load_fp4",
     "amla_pages_workspace_size", "amla_pages_copy", "amla_pages_free", "amla_pages_fork", "amla_pages_reserve", "amla_pages_compact",
+    "amla_cache_append", "amla_page_means", "amla_page_scores_workspace_size", "amla_page_scores", "amla_pages_select",
+    "amla_mla_decode_sparse_workspace_size", "amla_mla_decode_sparse", "amla_sparse_check_status",
 ]
 
 _lib = None
@@ -97,6 +99,22 @@ def lib() -> ctypes.CDLL:
         L.amla_pages_reserve.restype = i32
         L.amla_pages_compact.argtypes = [vp, i64, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]
         L.amla_pages_compact.restype = i32
+        L.amla_cache_append.argtypes = [i32, vp, i64, i32, vp, vp, f32, vp, vp, i32, i32, i32, vp, i32, vp, vp, i32, f32, i32, vp, i64, i64, vp, i64, i64, i32, vp]
+        L.amla_cache_append.restype = i32
+        L.amla_page_means.argtypes = [i32, vp, f32, vp, vp, vp, i32, i32, i32, i32, vp, vp]
+        L.amla_page_means.restype = i32
+        L.amla_page_scores_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+        L.amla_page_scores_workspace_size.restype = i32
+        L.amla_page_scores.argtypes = [vp, vp, vp, vp, f32, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+        L.amla_page_scores.restype = i32
+        L.amla_pages_select.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp]
+        L.amla_pages_select.restype = i32
+        L.amla_mla_decode_sparse_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+        L.amla_mla_decode_sparse_workspace_size.restype = i32
+        L.amla_mla_decode_sparse.argtypes = [i32, vp, vp, f32, vp, vp, vp, f32, i32, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.amla_mla_decode_sparse.restype = i32
+        L.amla_sparse_check_status.argtypes = [vp, vp]
+        L.amla_sparse_check_status.restype = i32
         L.amla_mla_decode_static.argtypes = [vp, vp, vp, vp, f32, i32, i32, i32, i32, i32, vp, vp, vp]
         L.amla_mla_decode_static.restype = i32
         L.amla_static_check_status.argtypes = [vp]

@@ -8,6 +8,7 @@
 #include "../../include/amla.h"
 #include "amla_common.cuh"
 #include "amla_fp4.cuh"
+#include "amla_select.cuh"
 
 namespace amla {
 cudaError_t launch_plan(const DecodeParams& prm, int* prefix_out, cudaStream_t stream);
@@ -432,6 +433,161 @@ extern "C" int amla_mla_decode(const void* q, const void* kv_cache, const int32_
   return amla_mla_decode_ex(q, kv_cache, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks,
                             max_blocks_per_seq, out, lse, workspace, workspace_bytes, cuda_stream,
                             AMLA_RESCALE_ALG2 | AMLA_LAZY(AMLA_DEFAULT_TAU));
+}
+
+namespace {
+
+// Table entries that a scoring takes: its blocks are counted in 31 bits, and there are up to 16 for 64 entries.
+constexpr long long kMostScored = 1 << 28;
+
+// A call's scoring scratch, in a workspace of its own: status | logits.
+size_t scores_bytes(int B, int Sq, int H, int width) { return kAlign + align_up(score_scratch_bytes(B, Sq, H, width)); }
+
+// The parts of a sparse call's workspace: the decode's (whose first 256 bytes have room for the scoring's status behind its own), the selected
+// table and lengths, the scores, and the scoring's scratch (neither of which a table no wider than `keep` needs).
+constexpr size_t kScoreStatusOff = sizeof(int);
+struct SparseLayout { size_t decode_bytes, table_off, lens_off, scores_off, scratch_off, total; };
+SparseLayout sparse_layout(int B, int Sq, int H, int width, int keep, int sms) {
+  const size_t tokens = static_cast<size_t>(B) * Sq;
+  const int nrb = (H + fp4_item_rows(H) - 1) / fp4_item_rows(H);    // (the 4-bit cache's kernel has the most items)
+  SparseLayout l;
+  l.decode_bytes = make_layout(B * Sq * nrb, sms).total;
+  l.table_off = align_up(l.decode_bytes);
+  l.lens_off = l.table_off + align_up(sizeof(int32_t) * tokens * keep);
+  l.scores_off = l.lens_off + align_up(sizeof(int32_t) * tokens);
+  l.scratch_off = l.scores_off + (width <= keep ? 0 : align_up(sizeof(float) * tokens * width));
+  l.total = l.scratch_off + (width <= keep ? 0 : align_up(score_scratch_bytes(B, Sq, H, width)));
+  return l;
+}
+
+int check_sparse_shape(int B, int Sq, int H, int width, int keep) {
+  int rc = check_shape(B, Sq, H, width);
+  if (rc != AMLA_OK) return rc;
+  if (keep <= 0) return AMLA_ERR_INVALID_ARG;
+  if (static_cast<long long>(B) * width > kMostScored) return AMLA_ERR_UNSUPPORTED;
+  if (static_cast<long long>(B) * Sq * 2 > (1ll << 24)) return AMLA_ERR_UNSUPPORTED;      // (items of the decode; rows of a grid)
+  return check_shape(B * Sq, 1, H, keep);
+}
+
+int check_selection(const int32_t* block_table, const int32_t* seqlens, int keep, int sink, int recent) {
+  if (!block_table || !seqlens || ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(seqlens)) & 3)) return AMLA_ERR_INVALID_ARG;
+  if (sink < 0 || recent < 1 || keep < 1 || static_cast<long long>(sink) + recent > keep) return AMLA_ERR_INVALID_ARG;
+  return AMLA_OK;
+}
+
+int device_of_call(int* device, int* sms) {
+  if (cudaGetDevice(device) != cudaSuccess) { cudaGetLastError(); return AMLA_ERR_CUDA; }
+  int cc = 0;
+  const int rc = sm_count_of(*device, sms, &cc);
+  return rc != AMLA_OK ? rc : cc != 10 ? AMLA_ERR_UNSUPPORTED : AMLA_OK;
+}
+
+int launched(cudaError_t err) {
+  if (err != cudaSuccess) { cudaGetLastError(); return AMLA_ERR_CUDA; }
+  return AMLA_OK;
+}
+
+}  // namespace
+
+extern "C" int amla_page_scores_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int device, size_t* bytes_out) {
+  if (!bytes_out || device < 0) return AMLA_ERR_INVALID_ARG;
+  const int rc = check_shape(B, Sq, H, max_blocks_per_seq);
+  if (rc != AMLA_OK) return rc;
+  if (static_cast<long long>(B) * max_blocks_per_seq > kMostScored) return AMLA_ERR_UNSUPPORTED;
+  *bytes_out = scores_bytes(B, Sq, H, max_blocks_per_seq);
+  return AMLA_OK;
+}
+
+extern "C" int amla_page_scores(const void* q, const void* means, const int32_t* block_table, const int32_t* seqlens, float softmax_scale, int B, int Sq, int H, int num_blocks,
+                                int max_blocks_per_seq, float* scores, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_arguments(q, means, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks, max_blocks_per_seq, scores, scores, workspace, 0);
+  if (rc != AMLA_OK) return rc;
+  if (static_cast<long long>(B) * max_blocks_per_seq > kMostScored) return AMLA_ERR_UNSUPPORTED;
+  if (workspace_bytes < scores_bytes(B, Sq, H, max_blocks_per_seq)) return AMLA_ERR_WORKSPACE;
+  int device = 0, sms = 0;
+  rc = device_of_call(&device, &sms);
+  if (rc != AMLA_OK) return rc;
+  char* ws = static_cast<char*>(workspace);
+  const ScoreParams p{static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(means), block_table, seqlens, softmax_scale * kLog2e, B, Sq, H, num_blocks,
+                      max_blocks_per_seq, reinterpret_cast<float*>(ws + kAlign), scores, reinterpret_cast<int*>(ws)};
+  return launched(launch_page_scores(p, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+extern "C" int amla_pages_select(const float* scores, const int32_t* block_table, const int32_t* seqlens, int B, int Sq, int max_blocks_per_seq, int keep, int sink, int recent,
+                                 int32_t* table, int32_t* lens, int32_t* chosen, void* cuda_stream) {
+  int rc = check_selection(block_table, seqlens, keep, sink, recent);
+  if (rc != AMLA_OK) return rc;
+  rc = check_sparse_shape(B, Sq, 1, max_blocks_per_seq, keep);
+  if (rc != AMLA_OK) return rc;
+  if ((!scores && max_blocks_per_seq > keep) || !table || !lens) return AMLA_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(scores) | reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(chosen)) & 3) return AMLA_ERR_INVALID_ARG;
+  return launched(launch_pages_select(SelectParams{scores, block_table, seqlens, B, Sq, max_blocks_per_seq, keep, sink, recent, table, lens, chosen, nullptr},
+                                      static_cast<cudaStream_t>(cuda_stream)));
+}
+
+extern "C" int amla_mla_decode_sparse_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int keep, int device, size_t* bytes_out) {
+  if (!bytes_out) return AMLA_ERR_INVALID_ARG;
+  int rc = check_sparse_shape(B, Sq, H, max_blocks_per_seq, keep);
+  if (rc != AMLA_OK) return rc;
+  int sms = 0, cc = 0;
+  rc = sm_count_of(device, &sms, &cc);
+  if (rc != AMLA_OK) return rc;
+  *bytes_out = sparse_layout(B, Sq, H, max_blocks_per_seq, keep, sms).total;
+  return AMLA_OK;
+}
+
+extern "C" int amla_mla_decode_sparse(int format, const void* q, const void* kv_cache, float kv_scale, const void* means, const int32_t* block_table, const int32_t* seqlens,
+                                      float softmax_scale, int B, int Sq, int H, int num_blocks, int max_blocks_per_seq, int keep, int sink, int recent, void* out, float* lse,
+                                      void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  g_last_launches = 0;
+  if (format != AMLA_CACHE_BF16 && format != AMLA_CACHE_E4M3 && format != AMLA_CACHE_FP4) return AMLA_ERR_INVALID_ARG;
+  int rc = check_selection(block_table, seqlens, keep, sink, recent);
+  if (rc != AMLA_OK) return rc;
+  rc = check_arguments(q, kv_cache, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks, max_blocks_per_seq, out, lse, workspace, 0);
+  if (rc != AMLA_OK) return rc;
+  rc = check_sparse_shape(B, Sq, H, max_blocks_per_seq, keep);
+  if (rc != AMLA_OK) return rc;
+  if (format != AMLA_CACHE_BF16 && !fp4_scale_ok(kv_scale)) return AMLA_ERR_INVALID_ARG;
+  const bool all = max_blocks_per_seq <= keep;
+  if (!all && (!means || (reinterpret_cast<uintptr_t>(means) & 15))) return AMLA_ERR_INVALID_ARG;
+  int device = 0, sms = 0;
+  rc = device_of_call(&device, &sms);
+  if (rc != AMLA_OK) return rc;
+  const SparseLayout lay = sparse_layout(B, Sq, H, max_blocks_per_seq, keep, sms);
+  if (workspace_bytes < lay.total) return AMLA_ERR_WORKSPACE;
+
+  char* ws = static_cast<char*>(workspace);
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  int32_t* table = reinterpret_cast<int32_t*>(ws + lay.table_off);
+  int32_t* lens = reinterpret_cast<int32_t*>(ws + lay.lens_off);
+  float* scores = reinterpret_cast<float*>(ws + lay.scores_off);
+  if (!all) {
+    const ScoreParams p{static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(means), block_table, seqlens, softmax_scale * kLog2e, B, Sq, H, num_blocks,
+                        max_blocks_per_seq, reinterpret_cast<float*>(ws + lay.scratch_off), scores, reinterpret_cast<int*>(ws + kScoreStatusOff)};
+    rc = launched(launch_page_scores(p, stream));
+    if (rc != AMLA_OK) return rc;
+  }
+  rc = launched(launch_pages_select(SelectParams{all ? nullptr : scores, block_table, seqlens, B, Sq, max_blocks_per_seq, keep, sink, recent, table, lens, nullptr,
+                                                all ? reinterpret_cast<int*>(ws + kScoreStatusOff) : nullptr}, stream));
+  if (rc != AMLA_OK) return rc;
+  const int front = all ? 1 : 3;
+  if (format == AMLA_CACHE_FP4)
+    rc = amla_mla_decode_fp4(q, kv_cache, kv_scale, table, lens, softmax_scale, B * Sq, 1, H, num_blocks, keep, out, lse, ws, lay.decode_bytes, cuda_stream);
+  else if (format == AMLA_CACHE_E4M3)      // (up to 128 rows: widened on their way in)
+    rc = decode_impl(q, nullptr, static_cast<const uint8_t*>(kv_cache), table, lens, softmax_scale * kv_scale, kv_scale, B * Sq, 1, H, num_blocks, keep, out, lse, ws,
+                     lay.decode_bytes, cuda_stream, AMLA_RESCALE_ALG2 | AMLA_LAZY(AMLA_DEFAULT_TAU));
+  else
+    rc = decode_impl(q, kv_cache, nullptr, table, lens, softmax_scale, 1.f, B * Sq, 1, H, num_blocks, keep, out, lse, ws, lay.decode_bytes, cuda_stream,
+                     AMLA_RESCALE_ALG2 | AMLA_LAZY(AMLA_DEFAULT_TAU));
+  g_last_launches += front;
+  return rc;
+}
+
+extern "C" int amla_sparse_check_status(const void* workspace, void* cuda_stream) {
+  if (!workspace) return AMLA_ERR_INVALID_ARG;
+  const int rc = amla_check_status(workspace, cuda_stream);
+  if (rc != AMLA_OK) return rc;
+  return amla_check_status(static_cast<const char*>(workspace) + kScoreStatusOff, cuda_stream);
 }
 
 extern "C" int amla_check_status(const void* workspace, void* cuda_stream) {

@@ -45,24 +45,6 @@ __device__ __forceinline__ Place place_of(const int32_t* starts, const int32_t* 
   return p;
 }
 
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-// x / step, inv = fl(1 / step) (0 for a group of zeros).  What is beyond E2M1's 6 by far saturates whatever its last bits are (and the
-// remainder of an infinity is a NaN).  The sign is x's, of a zero too (the remainder of -0 is +0).
-__device__ __forceinline__ float quotient(float x, float step, float inv) {
-  const float y = x * inv;
-  return copysignf(fabsf(y) < 16.f ? fmaf(fmaf(-y, step, x), inv, y) : y, x);
-}
-// low half: a, high half: b
-__device__ __forceinline__ uint32_t e2m1_byte(float a, float b) {
-  uint32_t r;
-  asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(r) : "f"(b), "f"(a));
-  return r;
-}
-
 // (Ordinary loads, here and of all pointers below: the kernel in front may still be writing the tokens when this one is placed.)
 // kWide: rows begin at 16 bytes, so that eight columns are one access
 template <bool kWide>

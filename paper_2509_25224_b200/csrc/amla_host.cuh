@@ -66,4 +66,19 @@ cudaError_t launch_serialized(Kernel kern, std::atomic<uint64_t>& done, int grid
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
+// The same for kernels without dynamic shared memory.
+template <typename... Params, typename... Args>
+cudaError_t launch_in_order(void (*kern)(Params...), dim3 grid, int threads, cudaStream_t stream, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, Params(args)...);
+}
+
 }  // namespace amla

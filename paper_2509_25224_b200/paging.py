@@ -1,5 +1,5 @@
-"""A paged cache's upkeep on the device: tokens into and out of a 4-bit cache, and copying, forking, freeing, reserving and
-compacting pages of any cache.  Argument checks and marshalling only; the work is done by the library's kernels, on the current
+"""A paged cache's upkeep on the device: tokens into a cache of any format (normed and rotated on the way, or as they are) and out of a 4-bit one, the
+means of full pages, and copying, forking, freeing, reserving and compacting pages of any cache.  Argument checks and marshalling only; the work is done by the library's kernels, on the current
 stream, and nothing is read back to the host.
 
 The books of a cache are int32 tensors: block_table [B, max_blocks], seqlens [B] and refs [num_blocks] (in how many table
@@ -15,6 +15,7 @@ from . import binding
 from .binding import AMLA_OK, AmlaError
 
 FP4_PAGE_BYTES = binding._FP4_PAGE_SHAPE[0]
+CACHE_BF16, CACHE_E4M3, CACHE_FP4 = 0, 1, 2
 
 _torch = _int = None
 _sizes: dict = {}                    # workspace bytes by (num_blocks, B)
@@ -149,6 +150,100 @@ def cache_load_fp4(kv_cache_fp4, kv_scale: float, block_table, seqlens, starts, 
           (kv_cache_fp4.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), starts.data_ptr(), B, blocks, width, out.data_ptr(), step, n),
           "amla_cache_load_fp4")
     return out
+
+
+def cache_format(cache) -> int:
+    """What a cache's pages hold (AMLA_CACHE_*), told from its shape and type: bf16 [num_blocks, 64, 576], uint8 of that shape (E4M3), uint8 [num_blocks, 20736] (4 bits)."""
+    shape = cache.shape
+    if len(shape) == 3 and shape[1] == 64 and shape[2] == 576:
+        if cache.dtype is _torch.bfloat16:
+            return CACHE_BF16
+        if cache.dtype is _torch.uint8:
+            return CACHE_E4M3
+    elif len(shape) == 2 and shape[1] == FP4_PAGE_BYTES and cache.dtype is _torch.uint8:
+        return CACHE_FP4
+    raise ValueError("the cache must be bfloat16 or uint8 [num_blocks, 64, 576], or uint8 [num_blocks, %d]" % FP4_PAGE_BYTES)
+
+
+def _batch(cache, starts, block_table, seqlens):
+    """(device index, format, sequences, entries a row, pages)"""
+    on = cache.get_device()
+    if on < 0:
+        raise ValueError("paging works on CUDA tensors, not tensors on " + str(cache.device))
+    fmt = cache_format(cache)
+    if not cache.is_contiguous():
+        raise ValueError("the cache must be contiguous")
+    _int32(starts, on, "starts")
+    _int32(block_table, on, "block_table")
+    _int32(seqlens, on, "seqlens")
+    if block_table.dim() != 2 or starts.dim() != 1 or seqlens.dim() != 1 or starts.numel() != block_table.shape[0] + 1 or seqlens.numel() != block_table.shape[0]:
+        raise ValueError("block_table is [B, max_blocks], seqlens [B], starts [B + 1]")
+    B, width = block_table.shape
+    return on, fmt, B, width, cache.shape[0]
+
+
+def _steps(t, on, columns, name):
+    """Strides (in elements) of a bf16 tensor [..., columns] whose columns are contiguous; an axis of at most one entry has none that matters."""
+    if t.dtype is not _torch.bfloat16 or t.get_device() != on or t.shape[-1] != columns or (t.numel() > 0 and t.stride(-1) != 1):
+        raise ValueError("%s must be bfloat16 [..., %d] with contiguous columns on the device of the cache" % (name, columns))
+    return [step if n > 1 else columns for step, n in zip(t.stride()[:-1], t.shape)]
+
+
+def cache_append(kv, starts, cache, kv_scale: float, block_table, seqlens, cos_sin, positions=None, norm_weight=None, eps: float = 1e-6, interleaved: bool = False, q_pe=None, q=None) -> None:
+    """New tokens into a cache of any format (cache_format), and their queries' position columns into place.
+
+    Rows starts[b] .. starts[b+1] - 1 of kv (bf16 [n, 576], perhaps a slice of wider rows) are the last tokens of sequence b, whose length seqlens[b] already
+    counts them.  Columns 0 .. 511 are normed where norm_weight (bf16 or fp32 [512]) is given, c * rsqrt(mean(c^2) + eps) * norm_weight; columns
+    512 .. 575 are rotated by the angles of the token's position (positions int32 [n]; None: its place in the sequence), whose cosines and sines
+    are a row of cos_sin (fp32 [n_positions, 64]).  interleaved: columns 2i, 2i+1 are a pair, else i, i+32.  q_pe (bf16 [n, H, 64], any strides)
+    is rotated into columns 512 .. 575 of q (bf16 [n, H, 576]).  ``include/amla.h`` says what happens to tokens without a place or a position."""
+    L = _ready()
+    on, fmt, B, width, blocks = _batch(cache, starts, block_table, seqlens)
+    if kv.dim() != 2:
+        raise ValueError("tokens are bfloat16 [n, 576]")
+    step, = _steps(kv, on, 576, "kv")
+    n = kv.shape[0]
+    if step < 576:
+        raise ValueError("rows of tokens must not overlap")
+    if cos_sin.dtype is not _torch.float32 or cos_sin.dim() != 2 or cos_sin.shape[1] != 64 or not cos_sin.is_contiguous() or cos_sin.get_device() != on:
+        raise ValueError("cos_sin must be a contiguous float32 [n_positions, 64] on the device of the cache")
+    at = 0
+    if positions is not None:
+        _int32(positions, on, "positions")
+        if positions.dim() != 1 or positions.numel() != n:
+            raise ValueError("positions is [n]")
+        at = positions.data_ptr()
+    weight = wide = 0
+    if norm_weight is not None:
+        wide = int(norm_weight.dtype is _torch.float32)
+        if not (wide or norm_weight.dtype is _torch.bfloat16) or norm_weight.shape != (512,) or not norm_weight.is_contiguous() or norm_weight.get_device() != on:
+            raise ValueError("norm_weight must be a contiguous bfloat16 or float32 [512] on the device of the cache")
+        weight = norm_weight.data_ptr()
+    if (q_pe is None) != (q is None):
+        raise ValueError("q_pe and q are given together, or neither")
+    from_q, to_q, H = (0, 0, 0), (0, 0, 0), 0
+    if q is not None:
+        if q_pe.dim() != 3 or q.dim() != 3 or q_pe.shape[:2] != q.shape[:2] or q.shape[0] != n:
+            raise ValueError("q_pe is [n, H, 64] and q [n, H, 576]")
+        H = q.shape[1]
+        from_q, to_q = (q_pe.data_ptr(), *_steps(q_pe, on, 64, "q_pe")), (q.data_ptr(), *_steps(q, on, 576, "q"))
+        if min(to_q[1:]) < 576:
+            raise ValueError("rows of q must not overlap")
+    _call(on, L.amla_cache_append,
+          (fmt, kv.data_ptr(), step, n, starts.data_ptr(), cache.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), B, blocks, width, cos_sin.data_ptr(),
+           cos_sin.shape[0], at, weight, wide, float(eps), int(interleaved), *from_q, *to_q, H), "amla_cache_append")
+
+
+def page_means(cache, kv_scale: float, block_table, seqlens, starts, n_tokens: int, means):
+    """means[page] (bf16 [num_blocks, 576]) = the mean key of every page that is filled by one of the tokens starts[b] .. starts[b+1] - 1, the last ones of
+    sequence b; n_tokens bounds starts[B].  The other pages' are left as they were.  Pages that were moved since (pages_compact, pages_copy): call it with all tokens."""
+    L = _ready()
+    on, fmt, B, width, blocks = _batch(cache, starts, block_table, seqlens)
+    if means.dtype is not _torch.bfloat16 or means.shape != (blocks, 576) or not means.is_contiguous() or means.get_device() != on:
+        raise ValueError("means must be a contiguous bfloat16 [num_blocks, 576] on the device of the cache")
+    _call(on, L.amla_page_means,
+          (fmt, cache.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), starts.data_ptr(), int(n_tokens), B, blocks, width, means.data_ptr()), "amla_page_means")
+    return means
 
 
 def pages_copy(cache, src, dst) -> None:
