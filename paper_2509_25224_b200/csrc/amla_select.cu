@@ -1,10 +1,14 @@
 // Which pages of a long context a query token attends to: scores from the pages' means, and the choice.
 #include "../../include/amla.h"
+#include "amla_fp4.cuh"
 #include "amla_host.cuh"
 #include "amla_select.cuh"
+#include "amla_sm100.cuh"
 #include "amla_tokens.cuh"
 
 namespace amla {
+
+using namespace sm100;
 
 namespace {
 
@@ -17,66 +21,174 @@ __device__ __forceinline__ int seen_by(const int32_t* seqlens, int b, int Sq, in
 // pages in front of the one that holds the token's own position
 __device__ __forceinline__ int candidates(int seen) { return seen > 0 ? (seen - 1) / kPage : 0; }
 
-constexpr int kTile = 64, kThreads = 256;
+// A block: 128 rows (query tokens' heads) times 128 pages.  The operands come through a ring of kStages places for 64 of the 576 columns of either.
+constexpr int kTileRows = 128, kTilePages = 128, kStatPages = 64, kThreads = 256;
+constexpr int kStages = 3, kChunks = kDqk / 64;
+constexpr uint32_t kOperandBytes = 128 * 128;                  // [128 rows][128 B], 128-byte swizzle
+constexpr uint32_t kOffPages = kStages * 2 * kOperandBytes, kOffBars = kOffPages + kTilePages * 4, kScoreSmem = kOffBars + 64;
+
+// The maximum of a row's logits over 64 pages, and the sum of 2^(logit - maximum)
+__host__ __device__ __forceinline__ int stats_of(int width) { return (width + kStatPages - 1) / kStatPages; }
+__device__ __forceinline__ float2* stats_at(const ScoreParams& p) { return reinterpret_cast<float2*>(p.logits + static_cast<size_t>(p.B) * p.Sq * p.H * logit_stride(p.width)); }
 
 }  // namespace
 
-// logits (base 2) of 64 rows and 64 pages
-__global__ void __launch_bounds__(kThreads) page_logits_kernel(const ScoreParams p) {
-  __shared__ float qs[16][kTile + 1], ms[16][kTile + 1];
-  __shared__ int pages[kTile];
+// Logits (base 2) of a block's rows and pages, and their statistics by 64 pages.
+__global__ void __launch_bounds__(kThreads, 2) page_logits_kernel(const ScoreParams p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, R = p.Sq * p.H;
+  const int tiles = (p.width + kTilePages - 1) / kTilePages, row_tiles = (R + kTileRows - 1) / kTileRows;
+  const int page0 = blockIdx.x % tiles * kTilePages, row0 = blockIdx.x / tiles % row_tiles * kTileRows, b = blockIdx.x / tiles / row_tiles;
+  const uint32_t base = smem_u32(smem), bars = base + kOffBars, tmem_slot = bars + 48;
+  int* pages = reinterpret_cast<int*>(smem + kOffPages);
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(bars + 8 * i, 1);
+    fence_mbar_init();
+  }
   behind_the_kernel_in_front();
-  const int tid = threadIdx.x, R = p.Sq * p.H, tiles = (p.width + kTile - 1) / kTile, row_tiles = (R + kTile - 1) / kTile;
-  const int page0 = blockIdx.x % tiles * kTile, row0 = blockIdx.x / tiles % row_tiles * kTile, b = blockIdx.x / tiles / row_tiles;
   if (blockIdx.x == 0 && tid == 0) *p.status = kStatusOk;
   const int most = candidates(seen_by(p.seqlens, b, p.Sq, p.Sq - 1, p.width));
   if (page0 >= most) return;
-  if (tid < kTile) pages[tid] = page0 + tid < most ? p.block_table[static_cast<size_t>(b) * p.width + page0 + tid] : -1;
-  float acc[4][4] = {};
-  const int tx = tid % 16, ty = tid / 16;
-  for (int k0 = 0; k0 < kDqk; k0 += 16) {
-    __syncthreads();
-    for (int i = tid; i < 16 * kTile; i += kThreads) {
-      const int k = i % 16, r = i / 16, page = pages[r];
-      qs[k][r] = row0 + r < R ? __bfloat162float(p.q[(static_cast<size_t>(b) * R + row0 + r) * kDqk + k0 + k]) : 0.f;
-      ms[k][r] = page >= 0 && page < p.num_blocks ? __bfloat162float(p.means[static_cast<size_t>(page) * kDqk + k0 + k]) : 0.f;
-    }
-    __syncthreads();
-    for (int k = 0; k < 16; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(qs[k][ty * 4 + i], ms[k][tx + 16 * j], acc[i][j]);
+  if (base & 1023u) {                                          // the swizzled tiles assume a 1024-byte aligned window
+    if (tid == 0) atomicExch(p.status, kStatusTimeout);
+    return;
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int r = row0 + ty * 4 + i, page = page0 + tx + 16 * j;
-      if (r < R && page < most) p.logits[(static_cast<size_t>(b) * R + r) * logit_stride(p.width) + page] = acc[i][j] * p.scale_log2;
+  if (wid == 0) { tmem_alloc(tmem_slot, kTilePages); tmem_relinquish(); }
+  if (tid < kTilePages) {
+    const int page = page0 + tid < most ? p.block_table[static_cast<size_t>(b) * p.width + page0 + tid] : -1;
+    pages[tid] = page < p.num_blocks ? page : -1;
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = ld_shared_b32(tmem_slot);
+
+  // a thread brings 16 bytes of every 32nd row of either operand
+  const int j = tid & 7, r0 = tid >> 3;
+  const __nv_bfloat16* q = p.q + (static_cast<size_t>(b) * R + row0) * kDqk + 8 * j;
+  const __nv_bfloat16* rows[4];
+  uint32_t live = 0, dst[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + 32 * i, page = pages[r];
+    rows[i] = p.means + static_cast<size_t>(max(page, 0)) * kDqk + 8 * j;
+    live |= (page >= 0 ? 1u : 0u) << i;
+    live |= (row0 + r < R ? 16u : 0u) << i;
+    dst[i] = base + sw128_offset(r, j);
+  }
+  auto load = [&](int c) {
+    const uint32_t at = c % kStages * 2 * kOperandBytes;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool mine = live >> (4 + i) & 1;
+      cp_async_16(dst[i] + at, mine ? q + (r0 + 32 * i) * kDqk + 64 * c : p.q, mine);
+      cp_async_16(dst[i] + at + kOperandBytes, rows[i] + 64 * c, live >> i & 1);
     }
+  };
+  bool ok = true;
+  for (int c = 0; c < kStages - 1; ++c) { load(c); cp_async_commit(); }
+#pragma unroll 1
+  for (int c = 0; c < kChunks; ++c) {
+    cp_async_wait_group<kStages - 2>();
+    fence_proxy_async_smem();
+    __syncthreads();
+    if (wid == 0 && elect_one()) {
+      constexpr uint32_t idesc = make_idesc_bf16(kTileRows, kTilePages, false, false), hi = smem_desc_hi_sw128(1024);
+      const uint32_t a = smem_desc_lo(base + c % kStages * 2 * kOperandBytes, 16), k = smem_desc_lo(base + c % kStages * 2 * kOperandBytes + kOperandBytes, 16);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) mma_ss(tmem, smem_desc_join(a + 2 * kk, hi), smem_desc_join(k + 2 * kk, hi), idesc, (c | kk) != 0 ? 1u : 0u);
+      mma_commit(bars + 8 * (c % kStages));
+    }
+    const int next = c + kStages - 1;
+    if (next < kChunks) {
+      if (c > 0 && ok) ok = mbar_wait(bars + 8 * (next % kStages), ((c - 1) / kStages) & 1);      // the products that read this place
+      if (ok) load(next);
+    }
+    cp_async_commit();                                         // (perhaps an empty group)
+  }
+  if (ok) ok = mbar_wait(bars + 8 * ((kChunks - 1) % kStages), ((kChunks - 1) / kStages) & 1);
+  __syncwarp();
+  tc_fence_after_sync();
+  if (__all_sync(0xffffffffu, ok)) {
+    // a thread has a row and 64 of the pages
+    const int quarter = wid & 3, half = wid >> 2, row = row0 + 32 * quarter + lane, first = page0 + kStatPages * half;
+    uint32_t v[2][32];
+    const uint32_t at = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + kStatPages * half;
+    tmem_ld_32x32b_x32(at, v[0]);
+    tmem_ld_32x32b_x32(at + 32, v[1]);
+    tmem_wait_ld();
+    if (row < R && first < most) {
+      const int count = candidates(seen_by(p.seqlens, b, p.Sq, row / p.H, p.width)) - first;
+      float* out = p.logits + (static_cast<size_t>(b) * R + row) * logit_stride(p.width) + first;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 64; ++i) {
+        const float l = __uint_as_float(v[i >> 5][i & 31]) * p.scale_log2;
+        v[i >> 5][i & 31] = __float_as_uint(l);
+        top = max_nan(top, i < count ? l : -INFINITY);
+      }
+      float sum = 0.f;
+      const float off = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < 64; ++i) sum += i < count ? ex2_approx(__uint_as_float(v[i >> 5][i & 31]) - off) : 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (4 * i < count) stg_128(out + 4 * i, v[i >> 3][4 * i & 31], v[i >> 3][(4 * i & 31) + 1], v[i >> 3][(4 * i & 31) + 2], v[i >> 3][(4 * i & 31) + 3]);
+      stats_at(p)[(static_cast<size_t>(b) * R + row) * stats_of(p.width) + first / kStatPages] = make_float2(top, sum);
+    }
+  } else if (lane == 0) {
+    atomicExch(p.status, kStatusTimeout);
+  }
+  cp_async_wait_all();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (wid == 0) tmem_dealloc(tmem, kTilePages);
 }
 
-// a block, a query token
-__global__ void __launch_bounds__(kThreads) page_mass_kernel(const ScoreParams p) {
-  __shared__ float lse[128];
+namespace {
+constexpr int kMassPages = 128, kMassThreads = 256;
+}  // namespace
+
+// A block: 128 pages of a query token, half of the heads by either half of the threads.
+__global__ void __launch_bounds__(kMassThreads) page_mass_kernel(const ScoreParams p) {
+  __shared__ float lse[128], part[kMassPages];
   behind_the_kernel_in_front();
-  const int tid = threadIdx.x, wid = tid / 32, lane = tid % 32, b = blockIdx.x / p.Sq, t = blockIdx.x % p.Sq;
-  const int count = candidates(seen_by(p.seqlens, b, p.Sq, t, p.width)), stride = logit_stride(p.width);
-  const float* logits = p.logits + (static_cast<size_t>(b) * p.Sq + t) * p.H * stride;
-  for (int h = wid; h < p.H; h += kThreads / 32) {
-    const float* row = logits + static_cast<size_t>(h) * stride;
+  const int tid = threadIdx.x, wid = tid / 32, lane = tid % 32, chunks = (p.width + kMassPages - 1) / kMassPages;
+  const int token = blockIdx.x / chunks, first = blockIdx.x % chunks * kMassPages, b = token / p.Sq, t = token % p.Sq;
+  const int count = candidates(seen_by(p.seqlens, b, p.Sq, t, p.width)), stride = logit_stride(p.width), stats = stats_of(count);
+  float* out = p.scores + static_cast<size_t>(token) * p.width;
+  if (first >= count) {
+    if (tid < kMassPages && first + tid < p.width) out[first + tid] = 0.f;
+    return;
+  }
+  for (int h = wid; h < p.H; h += kMassThreads / 32) {
+    const float2* row = stats_at(p) + (static_cast<size_t>(token) * p.H + h) * stats_of(p.width);
     float top = -INFINITY, sum = 0.f;
-    for (int i = lane; i < count; i += 32) top = fmaxf(top, row[i]);
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    for (int i = lane; i < count; i += 32) sum += exp2f(row[i] - top);
+    for (int i = lane; i < stats; i += 32) {
+      const float2 s = row[i];
+      const float m = max_nan(top, s.x);
+      sum = m == -INFINITY ? 0.f : sum * ex2_approx(top - m) + s.y * ex2_approx(s.x - m);
+      top = m;
+    }
+    float all = top;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) all = max_nan(all, __shfl_xor_sync(0xffffffffu, all, o));
+    sum = top == -INFINITY ? 0.f : sum * ex2_approx(top - all);
+#pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) lse[h] = top + log2f(sum);
+    if (lane == 0) lse[h] = all + log2f(sum);
   }
   __syncthreads();
-  float* out = p.scores + static_cast<size_t>(blockIdx.x) * p.width;
-  for (int i = tid; i < p.width; i += kThreads) {
-    float s = 0.f;
-    if (i < count)
-      for (int h = 0; h < p.H; ++h) s += exp2f(logits[static_cast<size_t>(h) * stride + i] - lse[h]);
-    out[i] = s;
+  const int at = tid % kMassPages, side = tid / kMassPages, page = first + at;
+  float s = 0.f;
+  if (page < count) {
+    const float* l = p.logits + static_cast<size_t>(token) * p.H * stride + page;
+#pragma unroll 8
+    for (int h = side; h < p.H; h += 2) s += ex2_approx(l[static_cast<size_t>(h) * stride] - lse[h]);
   }
+  if (side == 1) part[at] = s;
+  __syncthreads();
+  if (side == 0 && page < p.width) out[page] = s + part[at];
 }
 
 namespace {
@@ -194,13 +306,16 @@ __global__ void __launch_bounds__(kSelectThreads) pages_select_kernel(const Sele
   }
 }
 
-size_t score_scratch_bytes(int B, int Sq, int H, int width) { return sizeof(float) * static_cast<size_t>(B) * Sq * H * logit_stride(width); }
+size_t score_scratch_bytes(int B, int Sq, int H, int width) {
+  return static_cast<size_t>(B) * Sq * H * (sizeof(float) * logit_stride(width) + sizeof(float2) * stats_of(width));
+}
 
 cudaError_t launch_page_scores(const ScoreParams& p, cudaStream_t stream) {
+  static std::atomic<uint64_t> done{0};
   const int R = p.Sq * p.H;
-  cudaError_t err = launch_in_order(page_logits_kernel, dim3(p.B * ((p.width + kTile - 1) / kTile) * ((R + kTile - 1) / kTile)), kThreads, stream, p);
+  const cudaError_t err = launch_serialized(page_logits_kernel, done, p.B * ((p.width + kTilePages - 1) / kTilePages) * ((R + kTileRows - 1) / kTileRows), kThreads, kScoreSmem, stream, p);
   if (err != cudaSuccess) return err;
-  return launch_in_order(page_mass_kernel, dim3(p.B * p.Sq), kThreads, stream, p);
+  return launch_in_order(page_mass_kernel, dim3(p.B * p.Sq * ((p.width + kMassPages - 1) / kMassPages)), kMassThreads, stream, p);
 }
 
 cudaError_t launch_pages_select(const SelectParams& p, cudaStream_t stream) {
