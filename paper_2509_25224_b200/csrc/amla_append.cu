@@ -354,8 +354,8 @@ int check_books(const int32_t* starts, const void* cache, const int32_t* block_t
 
 template <int kFormat, bool kWide, bool kInterleaved>
 cudaError_t launch_append(const AppendParams& p, cudaStream_t stream) {
-  if (p.H > 32) return launch_in_order(append_kernel<kFormat, kWide, kInterleaved, 1>, dim3(p.tokens.n), kThreads, stream, p);
-  return launch_in_order(append_kernel<kFormat, kWide, kInterleaved, kWarps>, dim3((p.tokens.n + kWarps - 1) / kWarps), kThreads, stream, p);
+  if (p.H > 32) return launch_in_order(append_kernel<kFormat, kWide, kInterleaved, 1>, dim3(p.tokens.n), kThreads, 0, stream, p);
+  return launch_in_order(append_kernel<kFormat, kWide, kInterleaved, kWarps>, dim3((p.tokens.n + kWarps - 1) / kWarps), kThreads, 0, stream, p);
 }
 template <int kFormat>
 cudaError_t launch_append(const AppendParams& p, bool wide, bool interleaved, cudaStream_t stream) {
@@ -428,9 +428,9 @@ extern "C" int amla_page_means(int format, const void* kv_cache, float kv_scale,
   const int grid = (n_tokens + window - 1) / window;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(means);
-  const cudaError_t err = format == AMLA_CACHE_BF16   ? launch_in_order(page_means_kernel<AMLA_CACHE_BF16>, dim3(grid), kMeanThreads, stream, kv_cache, kv_scale, tokens, window, out)
-                          : format == AMLA_CACHE_E4M3 ? launch_in_order(page_means_kernel<AMLA_CACHE_E4M3>, dim3(grid), kMeanThreads, stream, kv_cache, kv_scale, tokens, window, out)
-                                                      : launch_in_order(page_means_kernel<AMLA_CACHE_FP4>, dim3(grid), kMeanThreads, stream, kv_cache, kv_scale, tokens, window, out);
+  const cudaError_t err = format == AMLA_CACHE_BF16   ? launch_in_order(page_means_kernel<AMLA_CACHE_BF16>, dim3(grid), kMeanThreads, 0, stream, kv_cache, kv_scale, tokens, window, out)
+                          : format == AMLA_CACHE_E4M3 ? launch_in_order(page_means_kernel<AMLA_CACHE_E4M3>, dim3(grid), kMeanThreads, 0, stream, kv_cache, kv_scale, tokens, window, out)
+                                                      : launch_in_order(page_means_kernel<AMLA_CACHE_FP4>, dim3(grid), kMeanThreads, 0, stream, kv_cache, kv_scale, tokens, window, out);
   if (err != cudaSuccess) { cudaGetLastError(); return AMLA_ERR_CUDA; }
   return AMLA_OK;
 }

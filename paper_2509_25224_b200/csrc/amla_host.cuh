@@ -40,10 +40,9 @@ inline bool encode_rows(EncodeTiledFn encode, CUtensorMap* map, const void* base
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Launches `kern` on `stream` with programmatic stream serialization.  The opt-in to large dynamic shared memory is per
-// device and per kernel: `done` remembers the devices that have it.
-template <typename Kernel, typename... Args>
-cudaError_t launch_serialized(Kernel kern, std::atomic<uint64_t>& done, int grid, int threads, uint32_t smem_bytes, cudaStream_t stream, const Args&... args) {
+// The opt-in to large dynamic shared memory is per device and per kernel: `done` remembers the devices that have it.
+template <typename Kernel>
+cudaError_t allow_shared(Kernel kern, std::atomic<uint64_t>& done, uint32_t smem_bytes) {
   int device = 0;
   cudaError_t err = cudaGetDevice(&device);
   if (err != cudaSuccess) return err;
@@ -53,8 +52,14 @@ cudaError_t launch_serialized(Kernel kern, std::atomic<uint64_t>& done, int grid
     if (err != cudaSuccess) return err;
     done.fetch_or(bit, std::memory_order_release);
   }
+  return cudaSuccess;
+}
+
+// Launches `kern` on `stream` with programmatic stream serialization.
+template <typename... Params, typename... Args>
+cudaError_t launch_in_order(void (*kern)(Params...), dim3 grid, int threads, uint32_t smem_bytes, cudaStream_t stream, const Args&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem_bytes;
   cfg.stream = stream;
@@ -63,22 +68,14 @@ cudaError_t launch_serialized(Kernel kern, std::atomic<uint64_t>& done, int grid
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, args...);
+  return cudaLaunchKernelEx(&cfg, kern, Params(args)...);
 }
 
-// The same for kernels without dynamic shared memory.
-template <typename... Params, typename... Args>
-cudaError_t launch_in_order(void (*kern)(Params...), dim3 grid, int threads, cudaStream_t stream, const Args&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, Params(args)...);
+// The same with `smem_bytes` of dynamic shared memory that the kernel always has.
+template <typename Kernel, typename... Args>
+cudaError_t launch_serialized(Kernel kern, std::atomic<uint64_t>& done, int grid, int threads, uint32_t smem_bytes, cudaStream_t stream, const Args&... args) {
+  const cudaError_t err = allow_shared(kern, done, smem_bytes);
+  return err != cudaSuccess ? err : launch_in_order(kern, dim3(grid), threads, smem_bytes, stream, args...);
 }
 
 }  // namespace amla
