@@ -440,13 +440,13 @@ namespace {
 // Table entries that a scoring takes: its blocks are counted in 31 bits, and there are up to 16 for 64 entries.
 constexpr long long kMostScored = 1 << 28;
 
-// A call's scoring scratch, in a workspace of its own: status | logits.
-size_t scores_bytes(int B, int Sq, int H, int width) { return kAlign + align_up(score_scratch_bytes(B, Sq, H, width)); }
+// What a scoring needs of a workspace: its status.
+constexpr size_t kScoresBytes = kAlign;
 
 // The parts of a sparse call's workspace: the decode's (whose first 256 bytes have room for the scoring's status behind its own), the selected
-// table and lengths, the scores, and the scoring's scratch (neither of which a table no wider than `keep` needs).
+// table and lengths, and the scores (which a table no wider than `keep` does not need).
 constexpr size_t kScoreStatusOff = sizeof(int);
-struct SparseLayout { size_t decode_bytes, table_off, lens_off, scores_off, scratch_off, total; };
+struct SparseLayout { size_t decode_bytes, table_off, lens_off, scores_off, total; };
 SparseLayout sparse_layout(int B, int Sq, int H, int width, int keep, int sms) {
   const size_t tokens = static_cast<size_t>(B) * Sq;
   const int nrb = (H + fp4_item_rows(H) - 1) / fp4_item_rows(H);    // (the 4-bit cache's kernel has the most items)
@@ -455,8 +455,7 @@ SparseLayout sparse_layout(int B, int Sq, int H, int width, int keep, int sms) {
   l.table_off = align_up(l.decode_bytes);
   l.lens_off = l.table_off + align_up(sizeof(int32_t) * tokens * keep);
   l.scores_off = l.lens_off + align_up(sizeof(int32_t) * tokens);
-  l.scratch_off = l.scores_off + (width <= keep ? 0 : align_up(sizeof(float) * tokens * width));
-  l.total = l.scratch_off + (width <= keep ? 0 : align_up(score_scratch_bytes(B, Sq, H, width)));
+  l.total = l.scores_off + (width <= keep ? 0 : align_up(sizeof(float) * tokens * width));
   return l;
 }
 
@@ -494,7 +493,7 @@ extern "C" int amla_page_scores_workspace_size(int B, int Sq, int H, int max_blo
   const int rc = check_shape(B, Sq, H, max_blocks_per_seq);
   if (rc != AMLA_OK) return rc;
   if (static_cast<long long>(B) * max_blocks_per_seq > kMostScored) return AMLA_ERR_UNSUPPORTED;
-  *bytes_out = scores_bytes(B, Sq, H, max_blocks_per_seq);
+  *bytes_out = kScoresBytes;
   return AMLA_OK;
 }
 
@@ -503,14 +502,14 @@ extern "C" int amla_page_scores(const void* q, const void* means, const int32_t*
   int rc = check_arguments(q, means, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks, max_blocks_per_seq, scores, scores, workspace, 0);
   if (rc != AMLA_OK) return rc;
   if (static_cast<long long>(B) * max_blocks_per_seq > kMostScored) return AMLA_ERR_UNSUPPORTED;
-  if (workspace_bytes < scores_bytes(B, Sq, H, max_blocks_per_seq)) return AMLA_ERR_WORKSPACE;
+  if (workspace_bytes < kScoresBytes) return AMLA_ERR_WORKSPACE;
   int device = 0, sms = 0;
   rc = device_of_call(&device, &sms);
   if (rc != AMLA_OK) return rc;
   char* ws = static_cast<char*>(workspace);
   const ScoreParams p{static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(means), block_table, seqlens, softmax_scale * kLog2e, B, Sq, H, num_blocks,
-                      max_blocks_per_seq, reinterpret_cast<float*>(ws + kAlign), scores, reinterpret_cast<int*>(ws)};
-  return launched(launch_page_scores(p, static_cast<cudaStream_t>(cuda_stream)));
+                      max_blocks_per_seq, scores, reinterpret_cast<int*>(ws)};
+  return launched(launch_page_scores(p, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 extern "C" int amla_pages_select(const float* scores, const int32_t* block_table, const int32_t* seqlens, int B, int Sq, int max_blocks_per_seq, int keep, int sink, int recent,
@@ -563,14 +562,14 @@ extern "C" int amla_mla_decode_sparse(int format, const void* q, const void* kv_
   float* scores = reinterpret_cast<float*>(ws + lay.scores_off);
   if (!all) {
     const ScoreParams p{static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(means), block_table, seqlens, softmax_scale * kLog2e, B, Sq, H, num_blocks,
-                        max_blocks_per_seq, reinterpret_cast<float*>(ws + lay.scratch_off), scores, reinterpret_cast<int*>(ws + kScoreStatusOff)};
-    rc = launched(launch_page_scores(p, stream));
+                        max_blocks_per_seq, scores, reinterpret_cast<int*>(ws + kScoreStatusOff)};
+    rc = launched(launch_page_scores(p, sms, stream));
     if (rc != AMLA_OK) return rc;
   }
   rc = launched(launch_pages_select(SelectParams{all ? nullptr : scores, block_table, seqlens, B, Sq, max_blocks_per_seq, keep, sink, recent, table, lens, nullptr,
                                                 all ? reinterpret_cast<int*>(ws + kScoreStatusOff) : nullptr}, stream));
   if (rc != AMLA_OK) return rc;
-  const int front = all ? 1 : 3;
+  const int front = all ? 1 : 2;
   if (format == AMLA_CACHE_FP4)
     rc = amla_mla_decode_fp4(q, kv_cache, kv_scale, table, lens, softmax_scale, B * Sq, 1, H, num_blocks, keep, out, lse, ws, lay.decode_bytes, cuda_stream);
   else if (format == AMLA_CACHE_E4M3)      // (up to 128 rows: widened on their way in)

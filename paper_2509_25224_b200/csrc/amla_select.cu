@@ -12,8 +12,6 @@ using namespace sm100;
 
 namespace {
 
-__host__ __device__ __forceinline__ int logit_stride(int width) { return (width + 31) / 32 * 32; }
-
 __device__ __forceinline__ int seen_by(const int32_t* seqlens, int b, int Sq, int t, int width) {
   const long long n = seqlens[b] < static_cast<long long>(width) * kPage ? seqlens[b] : width * kPage;
   return n - Sq + t + 1 > 0 ? static_cast<int>(n - Sq + t + 1) : 0;
@@ -21,212 +19,291 @@ __device__ __forceinline__ int seen_by(const int32_t* seqlens, int b, int Sq, in
 // pages in front of the one that holds the token's own position
 __device__ __forceinline__ int candidates(int seen) { return seen > 0 ? (seen - 1) / kPage : 0; }
 
-// A block of the products: 128 rows (query tokens' heads) times up to 256 pages.  The operands come through a ring of places for 64 of the 576 columns
-// of either, by the same warps that then make numbers of the products; one more warp issues those.
-constexpr int kTileRows = 128, kTilePages = 256, kLoadWarps = 8, kLoadThreads = 32 * kLoadWarps, kThreads = kLoadThreads + 32;
-constexpr int kStages = 4, kChunks = kDqk / 64;
-constexpr uint32_t kQBytes = kTileRows * 128, kPlaceBytes = kQBytes + kTilePages * 128;       // rows of 128 B, 128-byte swizzle
-constexpr uint32_t kOffPages = kStages * kPlaceBytes, kOffBars = kOffPages + kTilePages * 4, kScoreSmem = kOffBars + 128;
-enum { X_FULL = 0, X_EMPTY = kStages, X_DONE = 2 * kStages, X_NUM };
-static_assert(8 * X_NUM + 8 <= 128, "barrier area too small");
+// Scores.  An item is some query tokens of a sequence, as many as have 128 rows (a row: a head) between them; a cluster of up to eight blocks has an item,
+// a block a share of its pages.  It multiplies the rows by its pages' means, up to 256 pages at a time (a tile), keeps the logits of the
+// last two tiles in tensor memory, sends what it knows of every row (maximum and sum) to the others of the cluster and, with what they know,
+// makes shares of attention of its logits and adds them up over the heads.  Of more than two tiles the earlier ones are multiplied again.
+constexpr int kTileRows = 128, kTilePages = 256, kMostBlocks = 8;
+constexpr int kLoadWarps = 4, kLoadThreads = 32 * kLoadWarps, kSumWarps = 8, kSumThreads = 32 * kSumWarps, kMmaWarp = kLoadWarps + kSumWarps;
+constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr int kPart = 64;                                     // pages that a thread has in hand at a time
+constexpr int kMostStages = 9, kChunks = kDqk / 64;           // places of the ring, each for 64 of the 576 columns of either operand
+constexpr uint32_t kQBytes = kTileRows * 128;                 // rows of 128 B, 128-byte swizzle
+// Shared memory: the ring, in which a block of up to two tiles adds up its shares when all products are done ([128 rows][256 pages]); with more tiles the ring
+// is shorter and has [128 rows][128 pages] behind it.  Rows are 16 bytes longer than a multiple of 128: no two lanes of a store meet in a bank.
+constexpr uint32_t kWorkBytes = 219136, kFewBytes = kTileRows * (kTilePages / 2 + 4) * 4;
+constexpr uint32_t kOffStats = kWorkBytes, kOffKnown = kOffStats + kMostBlocks * kTileRows * 8, kOffLse = kOffKnown + kTileRows * 8;
+constexpr uint32_t kOffHalves = kOffLse + kTileRows * 4, kOffBars = kOffHalves + kTilePages / 2 * 4, kScoreSmem = kOffBars + 256;
+enum { X_FULL = 0, X_EMPTY = kMostStages, X_DONE = 2 * kMostStages, X_FREE = X_DONE + 2, X_STATS = X_FREE + 2, X_GIVE_UP, X_NUM };
+static_assert(8 * X_NUM + 8 <= 256 && kScoreSmem <= 232448 && kWorkBytes % 1024 == 0, "shared memory");
+static_assert(kTileRows * (kTilePages + 4) * 4 <= kWorkBytes && (kWorkBytes - kFewBytes) / (kQBytes + kTilePages * 128) >= 3, "ring");
 
-// What is known of a row's logits over kStatPages pages: their maximum, and the sum of 2^(logit - maximum).
-constexpr int kStatPages = 128;
-__host__ __device__ __forceinline__ int stats_of(int pages) { return (pages + kStatPages - 1) / kStatPages; }
-__device__ __forceinline__ float2* stats_at(const ScoreParams& p, int b, int stat) {
-  const size_t rows = static_cast<size_t>(p.Sq) * p.H;
-  return reinterpret_cast<float2*>(p.logits + p.B * rows * logit_stride(p.width)) + (static_cast<size_t>(b) * stats_of(p.width) + stat) * rows;
-}
+__host__ __device__ __forceinline__ int tokens_of_item(int Sq, int H) { return Sq < kTileRows / H ? Sq : kTileRows / H; }
 
-}  // namespace
-
-// Logits (base 2) of a block's rows and pages, and their statistics.
-__global__ void __launch_bounds__(kThreads, 1) page_logits_kernel(const ScoreParams p) {
-  extern __shared__ __align__(1024) uint8_t smem[];
-  const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, R = p.Sq * p.H;
-  const int tiles = (p.width + kTilePages - 1) / kTilePages, row_tiles = (R + kTileRows - 1) / kTileRows;
-  const int page0 = blockIdx.x % tiles * kTilePages, row0 = blockIdx.x / tiles % row_tiles * kTileRows, b = blockIdx.x / tiles / row_tiles;
-  const uint32_t base = smem_u32(smem), bars = base + kOffBars, tmem_slot = bars + 128 - 8;
-  auto bar = [&](int i) { return bars + 8u * i; };
-  int* pages = reinterpret_cast<int*>(smem + kOffPages);
-  if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(bar(X_FULL + i), kLoadThreads); mbar_init(bar(X_EMPTY + i), 1); }
-    mbar_init(bar(X_DONE), 1);
-    fence_mbar_init();
-  }
-  behind_the_kernel_in_front();
-  if (blockIdx.x == 0 && tid == 0) *p.status = kStatusOk;
-  const int most = candidates(seen_by(p.seqlens, b, p.Sq, p.Sq - 1, p.width));
-  if (page0 >= most) return;
-  if (base & 1023u) {                                          // the swizzled tiles assume a 1024-byte aligned window
-    if (tid == 0) atomicExch(p.status, kStatusTimeout);
-    return;
-  }
-  const int here = min(most - page0, kTilePages), n = (here + 15) / 16 * 16;      // pages, as products take them
-  if (wid == kLoadWarps) { tmem_alloc(tmem_slot, kTilePages); tmem_relinquish(); }
-  if (tid < kTilePages) {
-    const int page = tid < here ? p.block_table[static_cast<size_t>(b) * p.width + page0 + tid] : -1;
-    pages[tid] = page < p.num_blocks ? page : -1;
-  }
-  tc_fence_before_sync();
-  __syncthreads();
-  tc_fence_after_sync();
-  const uint32_t tmem = ld_shared_b32(tmem_slot);
-  bool ok = true;
-
-  if (wid == kLoadWarps) {
-    if (elect_one()) {
-      const uint32_t idesc = make_idesc_bf16(kTileRows, 16, false, false) + (static_cast<uint32_t>(n / 8 - 2) << 17);
-      constexpr uint32_t hi = smem_desc_hi_sw128(1024);
-#pragma unroll 1
-      for (int c = 0; c < kChunks && ok; ++c) {
-        const uint32_t place = c % kStages;
-        ok = mbar_wait(bar(X_FULL + place), (c / kStages) & 1);
-        if (!ok) break;
-        fence_proxy_async_smem();                              // the copies are ordinary writes
-        const uint32_t a = smem_desc_lo(base + place * kPlaceBytes, 16), k = smem_desc_lo(base + place * kPlaceBytes + kQBytes, 16);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) mma_ss(tmem, smem_desc_join(a + 2 * kk, hi), smem_desc_join(k + 2 * kk, hi), idesc, (c | kk) != 0 ? 1u : 0u);
-        mma_commit(bar(X_EMPTY + place));
-      }
-      mma_commit(bar(X_DONE));
-      if (!ok) { atomicExch(p.status, kStatusTimeout); mbar_wait(bar(X_DONE), 0); }
-    }
-    __syncwarp();
-  } else {
-    // a thread brings 16 bytes of every 32nd row of either operand (rows that there are not: whatever is there, in rows of the result that nobody reads)
-    const int j = tid & 7, r0 = tid >> 3;
-    const __nv_bfloat16* q = p.q + (static_cast<size_t>(b) * R + row0 + r0) * kDqk + 8 * j;
-    const int q_rows = min(R - row0, kTileRows) - r0;
-    int mine[kTilePages / 32];                                 // -1: outside the cache
-#pragma unroll
-    for (int i = 0; i < kTilePages / 32; ++i) mine[i] = pages[r0 + 32 * i];
-    const uint32_t dst = base + sw128_offset(r0, j);           // (32 rows further on the swizzle is the same)
-#pragma unroll 1
-    for (int c = 0; c < kChunks; ++c) {
-      const uint32_t place = c % kStages, to = dst + place * kPlaceBytes;
-      if (c >= kStages) {
-        ok = mbar_wait(bar(X_EMPTY + place), (c / kStages - 1) & 1);
-        if (!ok) break;
-      }
-#pragma unroll
-      for (int i = 0; i < kTileRows / 32; ++i)
-        if (32 * i < q_rows) cp_async_16(to + 4096 * i, q + 32 * i * kDqk + 64 * c, true);
-#pragma unroll
-      for (int i = 0; i < kTilePages / 32; ++i)
-        if (r0 + 32 * i < n) cp_async_16(to + kQBytes + 4096 * i, p.means + static_cast<size_t>(max(mine[i], 0)) * kDqk + 8 * j + 64 * c, mine[i] >= 0);
-      cp_async_arrive(bar(X_FULL + place));
-    }
-    ok = ok && mbar_wait(bar(X_DONE), 0);
-    ok = __all_sync(0xffffffffu, ok);
-    tc_fence_after_sync();
-    // a thread has a row and 128 of the pages, 64 at a time
-    const int quarter = wid & 3, half = wid >> 2, row = row0 + 32 * quarter + lane, first = kStatPages * half;
-    if (ok && first < here) {
-      const int token = min(row, R - 1) / p.H, count = row < R ? candidates(seen_by(p.seqlens, b, p.Sq, token, p.width)) - page0 - first : 0;
-      float* out = p.logits + (static_cast<size_t>(b) * R + row) * logit_stride(p.width) + page0 + first;
-      float top = -INFINITY, sum = 0.f;
-#pragma unroll 1
-      for (int part = 0; part < kStatPages; part += 64) {
-        if (first + part >= here) break;
-        uint32_t v[2][32];
-        const uint32_t at = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + first + part;
-        tmem_ld_32x32b_x32(at, v[0]);
-        tmem_ld_32x32b_x32(at + 32, v[1]);
-        tmem_wait_ld();
-        const int left = count - part;
-        float most_here = top;
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-          const float l = __uint_as_float(v[i >> 5][i & 31]) * p.scale_log2;
-          v[i >> 5][i & 31] = __float_as_uint(l);
-          most_here = max_nan(most_here, i < left ? l : -INFINITY);
-        }
-        const float off = most_here == -INFINITY ? 0.f : most_here;
-        sum *= ex2_approx(top - off);
-        top = most_here;
-#pragma unroll
-        for (int i = 0; i < 64; ++i) sum += i < left ? ex2_approx(__uint_as_float(v[i >> 5][i & 31]) - off) : 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (4 * i < left) stg_128(out + part + 4 * i, v[i >> 3][4 * i & 31], v[i >> 3][(4 * i & 31) + 1], v[i >> 3][(4 * i & 31) + 2], v[i >> 3][(4 * i & 31) + 3]);
-      }
-      if (row < R) stats_at(p, b, (page0 + first) / kStatPages)[row] = make_float2(top, sum);
-    }
-    if (!ok && lane == 0) atomicExch(p.status, kStatusTimeout);
-    cp_async_wait_all();
-  }
-  tc_fence_before_sync();
-  __syncthreads();
-  if (wid == kLoadWarps) tmem_dealloc(tmem, kTilePages);
-}
-
-namespace {
-
-constexpr int kMassPages = 128, kMassWarps = 16, kMassThreads = 32 * kMassWarps, kMostHeads = 128;
-constexpr int kMassHeads = kMostHeads / kMassWarps;           // of a warp
-
-// (top, sum) of two sets of logits together
+// (maximum, sum of 2^(logit - maximum)) of two sets of logits together
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
   const float top = max_nan(a.x, b.x), off = top == -INFINITY ? 0.f : top;
   return make_float2(top, a.y * ex2_approx(a.x - off) + b.y * ex2_approx(b.x - off));
 }
+template <int kBar, int kCount>
+__device__ __forceinline__ void meet() { asm volatile("bar.sync %0, %1;" ::"n"(kBar), "n"(kCount) : "memory"); }
+
+__device__ const uint4 zero_row[kDqk / 8] = {};
 
 }  // namespace
 
-// A block: 128 pages of a query token.  A warp brings all of them for every 16th head, four neighbouring pages a lane.
-__global__ void __launch_bounds__(kMassThreads) page_mass_kernel(const ScoreParams p) {
-  __shared__ float2 known[kMassThreads / kMostHeads][kMostHeads];
-  __shared__ float lse[kMostHeads];
-  __shared__ float4 sums[kMassWarps][32];
+__global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScoreParams p, int blocks) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
+  const int tokens_most = tokens_of_item(p.Sq, p.H), items = (p.Sq + tokens_most - 1) / tokens_most;
+  const int rank = blockIdx.x % blocks, item = blockIdx.x / blocks % items, b = blockIdx.x / blocks / items;
+  const int t0 = item * tokens_most, tokens = min(p.Sq - t0, tokens_most), rows = tokens * p.H;
+  const uint32_t base = smem_u32(smem), bars = base + kOffBars, tmem_slot = bars + 256 - 8;
+  auto bar = [&](int i) { return bars + 8u * i; };
+  if (tid == 0) {
+    for (int i = 0; i < kMostStages; ++i) { mbar_init(bar(X_FULL + i), kLoadThreads); mbar_init(bar(X_EMPTY + i), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar(X_DONE + i), 1); mbar_init(bar(X_FREE + i), kSumWarps); }
+    mbar_init(bar(X_STATS), 1);
+    mbar_init(bar(X_GIVE_UP), 1);
+    fence_mbar_init();
+    mbar_arrive_expect_tx(bar(X_STATS), blocks * kTileRows * 8);
+  }
+  if (wid == kMmaWarp) { tmem_alloc(tmem_slot, 2 * kTilePages); tmem_relinquish(); }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  cluster_arrive_relaxed();
+  const uint32_t tmem = ld_shared_b32(tmem_slot);
   behind_the_kernel_in_front();
-  const int tid = threadIdx.x, wid = tid / 32, lane = tid % 32, chunks = (p.width + kMassPages - 1) / kMassPages;
-  const int token = blockIdx.x / chunks, first = blockIdx.x % chunks * kMassPages, b = token / p.Sq, t = token % p.Sq;
-  const int count = candidates(seen_by(p.seqlens, b, p.Sq, t, p.width)), stride = logit_stride(p.width), stats = stats_of(count);
-  float* out = p.scores + static_cast<size_t>(token) * p.width;
-  if (first >= count) {
-    if (tid < kMassPages && first + tid < p.width) out[first + tid] = 0.f;
-    return;
-  }
-  float4 l[kMassHeads];
-  const int page = first + 4 * lane;
+  if (blockIdx.x == 0 && tid == 0) *p.status = kStatusOk;
+
+  const int most = candidates(seen_by(p.seqlens, b, p.Sq, t0 + tokens - 1, p.width));
+  const int share = ((most + blocks - 1) / blocks + 15) / 16 * 16, page0 = min(rank * share, most), here = min(share, most - page0);
+  const int tiles = (here + kTilePages - 1) / kTilePages, again = max(tiles - 2, 0);
+  // the k-th tile to be multiplied: all of them, then those that have left tensor memory, backwards
+  auto tile_of = [&](int k) { return k < tiles ? k : tiles - 3 - (k - tiles); };
+  const uint32_t place_bytes = kQBytes + (min(here, kTilePages) + 15) / 16 * 2048;
+  const uint32_t stages = min((kWorkBytes - (again ? kFewBytes : 0)) / place_bytes, static_cast<uint32_t>(kMostStages));
+  cluster_wait();
+  bool ok = (base & 1023u) == 0;                               // (the swizzled tiles assume a 1024-byte aligned window)
+
+  if (wid < kLoadWarps) {
+    // a thread brings 16 bytes of every 16th row of either operand (rows that there are not: whatever is there, in rows of the result that nobody reads)
+    const int j = tid & 7, r0 = tid >> 3;
+    const uint32_t dst = base + sw128_offset(r0, j);           // (16 rows further on the swizzle is the same)
+    const __nv_bfloat16* q = p.q + ((static_cast<size_t>(b) * p.Sq + t0) * p.H + r0) * kDqk + 8 * j;
+    const int rows_here = rows - r0;
+    uint32_t place = 0, par = 1;
+#pragma unroll 1
+    for (int k = 0; k < tiles + again && ok; ++k) {
+      const int first = tile_of(k) * kTilePages, n = (min(here - first, kTilePages) + 15) / 16 * 16;
+      const uint4* from[kTilePages / 16];                      // (a page outside the cache: zeros)
 #pragma unroll
-  for (int i = 0; i < kMassHeads; ++i) {
-    const int h = wid + kMassWarps * i;
-    if (h < p.H && page < count) l[i] = *reinterpret_cast<const float4*>(p.logits + (static_cast<size_t>(token) * p.H + h) * stride + page);
-  }
-  {
-    const int h = tid % kMostHeads, side = tid / kMostHeads;
-    float2 all = make_float2(-INFINITY, 0.f);
-    if (h < p.H) {
-#pragma unroll 4
-      for (int i = side; i < stats; i += kMassThreads / kMostHeads) all = join(all, stats_at(p, b, i)[t * p.H + h]);
+      for (int i = 0; i < kTilePages / 16; ++i) {
+        const int at = first + r0 + 16 * i, page = at < here ? p.block_table[static_cast<size_t>(b) * p.width + page0 + at] : -1;
+        from[i] = (page >= 0 && page < p.num_blocks ? reinterpret_cast<const uint4*>(p.means) + static_cast<size_t>(page) * (kDqk / 8) : zero_row) + j;
+      }
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {                      // (unrolled, so that an address is one that is at hand and a constant: a scheduler has one of these warps)
+        ok = ok && mbar_wait(bar(X_EMPTY + place), par);
+        if (!ok) break;
+        const uint32_t to = dst + place * place_bytes;
+#pragma unroll
+        for (int i = 0; i < kTileRows / 16; ++i)
+          if (16 * i < rows_here) cp_async_16(to + 2048 * i, q + 16 * i * kDqk + 64 * c);
+#pragma unroll
+        for (int i = 0; i < kTilePages / 16; ++i)
+          if (16 * i < n) cp_async_16(to + kQBytes + 2048 * i, from[i] + 8 * c);
+        cp_async_arrive(bar(X_FULL + place));
+        if (++place == stages) { place = 0; par ^= 1; }
+      }
     }
-    known[side][h] = all;
-  }
-  __syncthreads();
-  if (tid < p.H) {
-    const float2 all = join(join(known[0][tid], known[1][tid]), join(known[2][tid], known[3][tid]));
-    lse[tid] = all.x + log2f(all.y);
-  }
-  __syncthreads();
-  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    cp_async_wait_all();
+  } else if (wid == kMmaWarp) {
+    if (elect_one()) {
+      constexpr uint32_t hi = smem_desc_hi_sw128(1024);
+      uint32_t place = 0, par = 0, used[2] = {0, 0};
+#pragma unroll 1
+      for (int k = 0; k < tiles + again && ok; ++k) {
+        const int tile = tile_of(k), n = (min(here - tile * kTilePages, kTilePages) + 15) / 16 * 16;
+        const uint32_t idesc = make_idesc_bf16(kTileRows, 16, false, false) + (static_cast<uint32_t>(n / 8 - 2) << 17), buf = tile & 1, d = tmem + kTilePages * buf;
+        if (used[buf] > 0) ok = mbar_wait(bar(X_FREE + buf), (used[buf] - 1) & 1);
+        if (!ok) break;
+        ++used[buf];
+        tc_fence_after_sync();
+#pragma unroll 1
+        for (int c = 0; c < kChunks; ++c) {
+          ok = mbar_wait(bar(X_FULL + place), par);
+          if (!ok) break;
+          fence_proxy_async_smem();                            // the copies are ordinary writes
+          const uint32_t a = smem_desc_lo(base + place * place_bytes, 16), m = smem_desc_lo(base + place * place_bytes + kQBytes, 16);
 #pragma unroll
-  for (int i = 0; i < kMassHeads; ++i) {
-    const int h = wid + kMassWarps * i;
-    if (h < p.H && page < count) {
-      const float z = lse[h];
-      s.x += ex2_approx(l[i].x - z); s.y += ex2_approx(l[i].y - z); s.z += ex2_approx(l[i].z - z); s.w += ex2_approx(l[i].w - z);
+          for (int kk = 0; kk < 4; ++kk) mma_ss(d, smem_desc_join(a + 2 * kk, hi), smem_desc_join(m + 2 * kk, hi), idesc, (c | kk) != 0 ? 1u : 0u);
+          mma_commit(bar(X_EMPTY + place));
+          if (++place == stages) { place = 0; par ^= 1; }
+        }
+        if (ok) mma_commit(bar(X_DONE + buf));
+      }
+      if (!ok) {                                               // what has been issued ends before tensor memory is given back
+        mma_commit(bar(X_GIVE_UP));
+        mbar_wait(bar(X_GIVE_UP), 0);
+      }
+    }
+    __syncwarp();
+  } else {
+    // a thread has a row and 128 of a tile's pages, 64 at a time; when shares are added up, a page and half of the rows
+    const int quarter = wid & 3, half = (wid - kLoadWarps) >> 2, mine = (wid - kLoadWarps) * 32 + lane, row = 32 * quarter + lane;
+    const int token = min(row / p.H, tokens - 1), count = row < rows ? min(candidates(seen_by(p.seqlens, b, p.Sq, t0 + token, p.width)) - page0, here) : 0;
+    float* const out = p.scores + (static_cast<size_t>(b) * p.Sq + t0) * p.width;
+    for (int k = 0; k < tokens; ++k)                           // pages that are not scored
+      for (int i = candidates(seen_by(p.seqlens, b, p.Sq, t0 + k, p.width)) + rank * kSumThreads + mine; i < p.width; i += blocks * kSumThreads) out[static_cast<size_t>(k) * p.width + i] = 0.f;
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + kTilePages / 2 * half;
+    auto logits = [&](int tile, int part, uint32_t (&v)[2][32]) {
+      const uint32_t at = lanes + kTilePages * (tile & 1) + part;
+      tmem_ld_32x32b_x32(at, v[0]);
+      tmem_ld_32x32b_x32(at + 32, v[1]);
+      tmem_wait_ld();
+    };
+    const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
+    uint32_t done[2] = {0, 0};
+    auto wait_for = [&](int tile) {
+      const uint32_t buf = tile & 1;
+      ok = ok && mbar_wait(bar(X_DONE + buf), done[buf] & 1);
+      ok = __all_sync(0xffffffffu, ok);
+      ++done[buf];
+      tc_fence_after_sync();
+    };
+    auto give_back = [&](int tile) {
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(X_FREE + (tile & 1)));
+    };
+    float2 known = make_float2(-INFINITY, 0.f);
+#pragma unroll 1
+    for (int tile = 0; tile < tiles && ok; ++tile) {
+      wait_for(tile);
+      if (!ok) break;
+#pragma unroll 1
+      for (int part = 0; part < kTilePages / 2; part += kPart) {
+        const int first = tile * kTilePages + kTilePages / 2 * half + part;
+        if (first >= here) break;
+        uint32_t v[2][32];
+        logits(tile, part, v);
+        const int left = count - first;
+        // (the maximum of those that are numbers: one that is not makes the sum one)
+        float2 more = make_float2(-INFINITY, 0.f);
+        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < kPart; i += 2) {
+          float x, y;
+          unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1])), scale2), x, y);
+          if (i >= left) x = -INFINITY;
+          if (i + 1 >= left) y = -INFINITY;
+          v[i >> 5][i & 31] = __float_as_uint(x);
+          v[i >> 5][(i & 31) + 1] = __float_as_uint(y);
+          tops[i / 2 & 3] = fmax3(tops[i / 2 & 3], x, y);
+        }
+        more.x = fmaxf(fmax3(tops[0], tops[1], tops[2]), tops[3]);
+        const float off = more.x == -INFINITY ? 0.f : more.x;
+        const uint64_t off2 = pack_f32x2(-off, -off);
+        uint64_t sums[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < kPart; i += 2) {
+          float x, y;
+          unpack_f32x2(add_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1])), off2), x, y);
+          sums[i / 2 & 1] = add_f32x2(sums[i / 2 & 1], pack_f32x2(ex2_approx(x), ex2_approx(y)));
+        }
+        float x, y;
+        unpack_f32x2(add_f32x2(sums[0], sums[1]), x, y);
+        more.y = x + y;
+        known = join(known, more);
+      }
+      if (tile < again) give_back(tile);
+    }
+    float2* both = reinterpret_cast<float2*>(smem + kOffKnown);
+    float2* stats = reinterpret_cast<float2*>(smem + kOffStats);
+    float* lse = reinterpret_cast<float*>(smem + kOffLse);
+    if (half == 1) both[row] = known;
+    meet<1, kSumThreads>();
+    if (half == 0) {
+      known = join(known, both[row]);
+      const uint32_t at = base + kOffStats + (rank * kTileRows + row) * 8;
+      for (int i = 0; i < blocks; ++i) st_async_v2(map_to_cta(at, i), __float_as_uint(known.x), __float_as_uint(known.y), map_to_cta(bar(X_STATS), i));
+      ok = __all_sync(0xffffffffu, mbar_wait<true>(bar(X_STATS), 0) && ok);
+      float2 all = stats[row];
+      for (int i = 1; i < blocks; ++i) all = join(all, stats[i * kTileRows + row]);
+      lse[row] = all.x + log2f(all.y);
+    }
+    meet<1, kSumThreads>();
+    const uint64_t off2 = pack_f32x2(-lse[row], -lse[row]);
+    // a round: all of a tile's pages where there is room, else 64 of either half
+    const int rounds = again ? 2 : 1, wide = kTilePages / rounds, stride = wide + 4;
+    float* const shares = reinterpret_cast<float*>(smem + (again ? kWorkBytes - kFewBytes : 0));
+    float* const halves = reinterpret_cast<float*>(smem + kOffHalves);
+    const int column = mine % wide, side = mine / wide;
+#pragma unroll 1
+    for (int tile = tiles - 1; tile >= 0; --tile) {
+      if (tile < again) wait_for(tile);
+#pragma unroll 1
+      for (int round = 0; round < rounds; ++round) {
+#pragma unroll 1
+        for (int part = round * kPart; part < (rounds == 1 ? kTilePages / 2 : (round + 1) * kPart); part += kPart) {
+          const int first = tile * kTilePages + kTilePages / 2 * half + part, left = count - first;
+          if (first >= here || !ok) break;
+          float* to = shares + row * stride + wide / 2 * half + (rounds == 1 ? part : 0);
+          uint32_t v[2][32];
+          logits(tile, part, v);
+#pragma unroll
+          for (int i = 0; i < kPart; i += 4) {
+            float e[4];
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {
+              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][(i & 31) + k]), __uint_as_float(v[i >> 5][(i & 31) + k + 1])), scale2, off2), e[k], e[k + 1]);
+              e[k] = i + k < left ? ex2_approx(e[k]) : 0.f;
+              e[k + 1] = i + k + 1 < left ? ex2_approx(e[k + 1]) : 0.f;
+            }
+            *reinterpret_cast<float4*>(to + i) = make_float4(e[0], e[1], e[2], e[3]);
+          }
+        }
+        meet<1, kSumThreads>();
+        // (of a round of two halves of 64 pages, the second is 128 pages further on)
+        const int at = tile * kTilePages + (rounds == 1 ? column : round * kPart + column + (column >= kPart ? kPart : 0));
+        const float* const from = shares + column;
+        auto sum = [&](int r, int end) {
+          float s[4] = {0.f, 0.f, 0.f, 0.f};
+          for (; r + 16 <= end; r += 16) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i & 3] += from[(r + i) * stride];
+          }
+          for (; r < end; ++r) s[0] += from[r * stride];
+          return (s[0] + s[1]) + (s[2] + s[3]);
+        };
+        if (rounds == 1) {
+          if (at < here)
+            for (int k = 0; k < tokens; ++k) out[static_cast<size_t>(k) * p.width + page0 + at] = sum(k * p.H, (k + 1) * p.H);
+        } else if (tokens == 1) {
+          const int middle = (p.H + 1) / 2;
+          const float s = side == 0 ? sum(0, middle) : sum(middle, p.H);
+          if (side == 1) halves[column] = s;
+          meet<1, kSumThreads>();
+          if (side == 0 && at < here) out[page0 + at] = s + halves[column];
+        } else {
+          for (int k = side; k < tokens; k += 2) {
+            const float s = sum(k * p.H, (k + 1) * p.H);
+            if (at < here) out[static_cast<size_t>(k) * p.width + page0 + at] = s;
+          }
+        }
+        if (tile > 0 || round + 1 < rounds) meet<1, kSumThreads>();
+      }
+      if (tile >= 2) give_back(tile);
     }
   }
-  sums[wid][lane] = s;
+  if (!ok) atomicExch(p.status, kStatusTimeout);
+  tc_fence_before_sync();
   __syncthreads();
-  if (tid < kMassPages && first + tid < p.width) {
-    float all = 0.f;
-#pragma unroll
-    for (int w = 0; w < kMassWarps; ++w) all += reinterpret_cast<const float*>(sums[w])[tid];
-    out[first + tid] = first + tid < count ? all : 0.f;
-  }
+  if (wid == kMmaWarp) tmem_dealloc(tmem, 2 * kTilePages);
+  cluster_arrive_relaxed();                                    // (who gave up must not be gone when another's statistics arrive)
+  cluster_wait();
 }
 
 namespace {
@@ -353,16 +430,33 @@ __global__ void __launch_bounds__(kSelectThreads) pages_select_kernel(const Sele
   }
 }
 
-size_t score_scratch_bytes(int B, int Sq, int H, int width) {
-  return static_cast<size_t>(B) * Sq * H * (sizeof(float) * logit_stride(width) + sizeof(float2) * stats_of(width));
+// Blocks in a cluster: as many as there are SMs for, but none that would have less than 64 pages of the longest sequence.
+int score_blocks(const ScoreParams& p, int sms) {
+  const long long items = static_cast<long long>(p.B) * ((p.Sq + tokens_of_item(p.Sq, p.H) - 1) / tokens_of_item(p.Sq, p.H));
+  int blocks = 1;
+  while (blocks < kMostBlocks && items * 2 * blocks <= sms && p.width > 64 * blocks) blocks *= 2;
+  return blocks;
 }
 
-cudaError_t launch_page_scores(const ScoreParams& p, cudaStream_t stream) {
+cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t stream) {
   static std::atomic<uint64_t> done{0};
-  const int R = p.Sq * p.H;
-  const cudaError_t err = launch_serialized(page_logits_kernel, done, p.B * ((p.width + kTilePages - 1) / kTilePages) * ((R + kTileRows - 1) / kTileRows), kThreads, kScoreSmem, stream, p);
+  const int blocks = score_blocks(p, sms), items = (p.Sq + tokens_of_item(p.Sq, p.H) - 1) / tokens_of_item(p.Sq, p.H);
+  const cudaError_t err = allow_shared(page_scores_kernel, done, kScoreSmem);
   if (err != cudaSuccess) return err;
-  return launch_in_order(page_mass_kernel, dim3(p.B * p.Sq * ((p.width + kMassPages - 1) / kMassPages)), kMassThreads, 0, stream, p);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.B * items * blocks);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kScoreSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = blocks;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, blocks);
 }
 
 cudaError_t launch_pages_select(const SelectParams& p, cudaStream_t stream) {

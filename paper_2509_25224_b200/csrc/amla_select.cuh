@@ -12,7 +12,6 @@ struct ScoreParams {
   const int32_t* seqlens;        // [B]
   float scale_log2;
   int B, Sq, H, num_blocks, width;
-  float* logits;                 // scratch
   float* scores;                 // [B, Sq, width]
   int* status;
 };
@@ -28,8 +27,7 @@ struct SelectParams {
   int* clear;                    // a status word that no scoring in front has set, or null
 };
 
-size_t score_scratch_bytes(int B, int Sq, int H, int width);
-cudaError_t launch_page_scores(const ScoreParams& p, cudaStream_t stream);
+cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t stream);
 cudaError_t launch_pages_select(const SelectParams& p, cudaStream_t stream);
 
 }  // namespace amla
