@@ -19,24 +19,25 @@ __device__ __forceinline__ int seen_by(const int32_t* seqlens, int b, int Sq, in
 // pages in front of the one that holds the token's own position
 __device__ __forceinline__ int candidates(int seen) { return seen > 0 ? (seen - 1) / kPage : 0; }
 
-// Scores.  An item is some query tokens of a sequence, as many as have 128 rows (a row: a head) between them; a cluster of up to eight blocks has an item,
+// Scores.  An item is some query tokens of a sequence, as many as have 128 rows (a row: a head) between them; a cluster of up to sixteen blocks has an item,
 // a block a share of its pages.  It multiplies the rows by its pages' means, up to 256 pages at a time (a tile), keeps the logits of the
 // last two tiles in tensor memory, sends what it knows of every row (maximum and sum) to the others of the cluster and, with what they know,
 // makes shares of attention of its logits and adds them up over the heads.  Of more than two tiles the earlier ones are multiplied again.
-constexpr int kTileRows = 128, kTilePages = 256, kMostBlocks = 8;
+constexpr int kTileRows = 128, kTilePages = 256, kMostBlocks = 16;
 constexpr int kLoadWarps = 4, kLoadThreads = 32 * kLoadWarps, kSumWarps = 8, kSumThreads = 32 * kSumWarps, kMmaWarp = kLoadWarps + kSumWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 1);
 constexpr int kPart = 64;                                     // pages that a thread has in hand at a time
 constexpr int kMostStages = 9, kChunks = kDqk / 64;           // places of the ring, each for 64 of the 576 columns of either operand
 constexpr uint32_t kQBytes = kTileRows * 128;                 // rows of 128 B, 128-byte swizzle
 // Shared memory: the ring, in which a block of up to two tiles adds up its shares when all products are done ([128 rows][256 pages]); with more tiles the ring
-// is shorter and has [128 rows][128 pages] behind it.  Rows are 16 bytes longer than a multiple of 128: no two lanes of a store meet in a bank.
-constexpr uint32_t kWorkBytes = 219136, kFewBytes = kTileRows * (kTilePages / 2 + 4) * 4;
-constexpr uint32_t kOffStats = kWorkBytes, kOffKnown = kOffStats + kMostBlocks * kTileRows * 8, kOffLse = kOffKnown + kTileRows * 8;
+// is shorter and has [128 rows][128 pages] behind it.  Rows are 16 bytes longer than a multiple of 128: no two lanes of a store meet in a bank.  The others'
+// statistics come in at the end, which is no place of the ring, and have been read when shares are added up.
+constexpr uint32_t kWorkBytes = 227328, kStatsBytes = kMostBlocks * kTileRows * 8, kFewBytes = kTileRows * (kTilePages / 2 + 4) * 4;
+constexpr uint32_t kOffStats = kWorkBytes - kStatsBytes, kOffKnown = kWorkBytes, kOffLse = kOffKnown + kTileRows * 8;
 constexpr uint32_t kOffHalves = kOffLse + kTileRows * 4, kOffBars = kOffHalves + kTilePages / 2 * 4, kScoreSmem = kOffBars + 256;
 enum { X_FULL = 0, X_EMPTY = kMostStages, X_DONE = 2 * kMostStages, X_FREE = X_DONE + 2, X_STATS = X_FREE + 2, X_GIVE_UP, X_NUM };
 static_assert(8 * X_NUM + 8 <= 256 && kScoreSmem <= 232448 && kWorkBytes % 1024 == 0, "shared memory");
-static_assert(kTileRows * (kTilePages + 4) * 4 <= kWorkBytes && (kWorkBytes - kFewBytes) / (kQBytes + kTilePages * 128) >= 3, "ring");
+static_assert(kTileRows * (kTilePages + 4) * 4 <= kOffStats && kStatsBytes <= kFewBytes && (kWorkBytes - kFewBytes) / (kQBytes + kTilePages * 128) >= 3, "ring");
 
 __host__ __device__ __forceinline__ int tokens_of_item(int Sq, int H) { return Sq < kTileRows / H ? Sq : kTileRows / H; }
 
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
   // the k-th tile to be multiplied: all of them, then those that have left tensor memory, backwards
   auto tile_of = [&](int k) { return k < tiles ? k : tiles - 3 - (k - tiles); };
   const uint32_t place_bytes = kQBytes + (min(here, kTilePages) + 15) / 16 * 2048;
-  const uint32_t stages = min((kWorkBytes - (again ? kFewBytes : 0)) / place_bytes, static_cast<uint32_t>(kMostStages));
+  const uint32_t stages = min((kWorkBytes - (again ? kFewBytes : kStatsBytes)) / place_bytes, static_cast<uint32_t>(kMostStages));
   cluster_wait();
   bool ok = (base & 1023u) == 0;                               // (the swizzled tiles assume a 1024-byte aligned window)
 
@@ -430,25 +431,14 @@ __global__ void __launch_bounds__(kSelectThreads) pages_select_kernel(const Sele
   }
 }
 
-// Blocks in a cluster: as many as there are SMs for, but none that would have less than 64 pages of the longest sequence.
-int score_blocks(const ScoreParams& p, int sms) {
-  const long long items = static_cast<long long>(p.B) * ((p.Sq + tokens_of_item(p.Sq, p.H) - 1) / tokens_of_item(p.Sq, p.H));
-  int blocks = 1;
-  while (blocks < kMostBlocks && items * 2 * blocks <= sms && p.width > 64 * blocks) blocks *= 2;
-  return blocks;
-}
+namespace {
 
-cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t stream) {
-  static std::atomic<uint64_t> done{0};
-  const int blocks = score_blocks(p, sms), items = (p.Sq + tokens_of_item(p.Sq, p.H) - 1) / tokens_of_item(p.Sq, p.H);
-  const cudaError_t err = allow_shared(page_scores_kernel, done, kScoreSmem);
-  if (err != cudaSuccess) return err;
+cudaLaunchConfig_t score_config(int clusters, int blocks, cudaStream_t stream, cudaLaunchAttribute (&attr)[2]) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.B * items * blocks);
+  cfg.gridDim = dim3(clusters * blocks);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kScoreSmem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -456,6 +446,47 @@ cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t strea
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
+  return cfg;
+}
+
+// How many clusters of sixteen blocks the current device has room for (a property of it, looked up once).
+int clusters_of_16() {
+  static std::atomic<int> known[64];                           // one more than the number
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); return 0; }
+  std::atomic<int>& k = known[device & 63];
+  if (k.load(std::memory_order_acquire) == 0) {
+    int n = 0;
+    cudaLaunchAttribute attr[2];
+    const cudaLaunchConfig_t cfg = score_config(1, 16, nullptr, attr);
+    if (cudaFuncSetAttribute(page_scores_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, page_scores_kernel, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    k.store(n + 1, std::memory_order_release);
+  }
+  return k.load(std::memory_order_acquire) - 1;
+}
+
+// Blocks in a cluster: as many as there are SMs for, but none that would have less than 64 pages of the longest sequence, and sixteen only where
+// that leaves no block with more than a tile, or fewer tiles, and all clusters have room.
+int score_blocks(int items, int width, int sms) {
+  int blocks = 1;
+  while (blocks < 8 && static_cast<long long>(items) * 2 * blocks <= sms && width > 64 * blocks) blocks *= 2;
+  if (blocks == 8 && width > 8 * kTilePages && items <= sms / 16 && items <= clusters_of_16()) blocks = 16;
+  return blocks;
+}
+
+}  // namespace
+
+cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t stream) {
+  static std::atomic<uint64_t> done{0};
+  const int items = p.B * ((p.Sq + tokens_of_item(p.Sq, p.H) - 1) / tokens_of_item(p.Sq, p.H));
+  const cudaError_t err = allow_shared(page_scores_kernel, done, kScoreSmem);
+  if (err != cudaSuccess) return err;
+  const int blocks = score_blocks(items, p.width, sms);
+  cudaLaunchAttribute attr[2];
+  const cudaLaunchConfig_t cfg = score_config(items, blocks, stream, attr);
   return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, blocks);
 }
 
