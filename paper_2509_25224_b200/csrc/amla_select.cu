@@ -309,8 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
 
 namespace {
 
-constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32;
-constexpr int kHeldKeys = 32768;                               // scores whose order is kept in shared memory; of longer rows it is worked out again each time
+constexpr int kHeldPages = 24576;                              // up to so many pages a row's scores, as their order, and what is chosen of them are kept in shared memory
 
 // A number's place in the order of scores: larger for larger ones, the same for both zeros, that of -infinity for a NaN.
 __device__ __forceinline__ uint32_t order_of(float f) {
@@ -323,16 +322,23 @@ __device__ __forceinline__ uint32_t order_of(float f) {
 
 // A block, a query token.  The scores' order is looked at eight bits at a time, from the top: how many of those that agree with the bits found
 // so far have which next eight; the one that is looked for lies in one of these 256, and if all of those are wanted the bits suffice.
-template <bool kHeld>
+template <int kSelectThreads, bool kHeld>
 __global__ void __launch_bounds__(kSelectThreads) pages_select_kernel(const SelectParams p) {
-  extern __shared__ uint32_t held_keys[];
-  __shared__ int hist[256];
-  __shared__ int found[3];                                     // next eight bits, wanted among those, how many there are
-  __shared__ int2 totals[kSelectWarps];
-  behind_the_kernel_in_front();
+  extern __shared__ uint32_t held_keys[];                      // [width], then positions of the chosen pages [keep]
+  __shared__ __align__(16) int counts[4][256];                 // a table for each of the four times, the largest eight bits first
+  __shared__ int4 found;                                       // the next eight bits, how many are wanted of those that have them, how many there are
+  __shared__ int2 totals[kSelectThreads / 32];
+  __shared__ uint2 kinds[kSelectThreads];                      // of 32 pages each: which are taken anyway, and which agree
   const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, row = blockIdx.x, b = row / p.Sq, t = row % p.Sq;
-  const int seen = seen_by(p.seqlens, b, p.Sq, t, p.width), count = (seen + kPage - 1) / kPage;
+  for (int i = tid; i < 1024; i += kSelectThreads) reinterpret_cast<int*>(counts)[i] = 0;
+  behind_the_kernel_in_front();
+  const float* scores = p.scores + static_cast<size_t>(row) * p.width;
   const int32_t* entries = p.block_table + static_cast<size_t>(b) * p.width;
+  const int seen = seen_by(p.seqlens, b, p.Sq, t, p.width), count = (seen + kPage - 1) / kPage;
+  if (kHeld && p.width > p.keep) {                             // (all of the row, since the length is on its way)
+#pragma unroll 4
+    for (int i = tid; i < p.width; i += kSelectThreads) held_keys[i] = order_of(scores[i]);
+  }
   int32_t* table = p.table + static_cast<size_t>(row) * p.keep;
   int32_t* chosen = p.chosen ? p.chosen + static_cast<size_t>(row) * p.keep : nullptr;
   const int kept = min(count, p.keep);
@@ -349,85 +355,97 @@ __global__ void __launch_bounds__(kSelectThreads) pages_select_kernel(const Sele
     }
     return;
   }
-  const float* scores = p.scores + static_cast<size_t>(row) * p.width;
   const int first = p.sink, end = count - p.recent;            // the others; more than are wanted
-  auto key = [&](int i) { return kHeld ? held_keys[i - first] : order_of(scores[i]); };
-  if (kHeld) {
-    for (int i = first + tid; i < end; i += kSelectThreads) held_keys[i - first] = order_of(scores[i]);
-  }
+  auto key = [&](int i) { return kHeld ? held_keys[i] : order_of(scores[i]); };
   int left = p.keep - p.sink - p.recent, shift = 32;           // wanted of those that agree in the bits from `shift` on
   uint32_t prefix = 0;
+  __syncthreads();
   if (left > 0) {
+    int there;
     do {
       shift -= 8;
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
+      int* const table_of = counts[shift >> 3];
+#pragma unroll 1
       for (int i = first + tid; i < end; i += kSelectThreads) {
         const uint32_t k = key(i);
-        if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&hist[(k >> shift) & 255], 1);
+        if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&table_of[~(k >> shift) & 255], 1);
       }
       __syncthreads();
       if (wid == 0) {                                          // lane 0 has the largest eight
-        int mine[8], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { mine[i] = hist[255 - 8 * lane - i]; sum += mine[i]; }
+        const int4 a = *reinterpret_cast<const int4*>(table_of + 8 * lane), c = *reinterpret_cast<const int4*>(table_of + 8 * lane + 4);
+        const int mine[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w}, sum = ((a.x + a.y) + (a.z + a.w)) + ((c.x + c.y) + (c.z + c.w));
         int above = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, above, o); if (lane >= o) above += x; }
         above -= sum;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (above < left && left <= above + mine[i]) { found[0] = 255 - 8 * lane - i; found[1] = left - above; found[2] = mine[i]; }
+          if (above < left && left <= above + mine[i]) found = make_int4(255 - 8 * lane - i, left - above, mine[i], 0);
           above += mine[i];
         }
       }
       __syncthreads();
-      prefix |= static_cast<uint32_t>(found[0]) << shift;
-      left = found[1];
-    } while (shift > 0 && left < found[2]);
+      prefix |= static_cast<uint32_t>(found.x) << shift;
+      left = found.y;
+      there = found.z;
+    } while (shift > 0 && left < there);
   } else {
-    __syncthreads();
     shift = 0;
-    prefix = 0xffffffffu;                                      // (no score is)
+    prefix = 0xfffffffeu;                                      // above every score, below the pages that are taken anyway
   }
   prefix >>= shift;
-  // those above, and the first `left` of those that agree: a warp goes through neighbouring pages, 32 at a time
-  const int each = (count + kSelectThreads - 1) / kSelectThreads * 32, lo = min(wid * each, count), hi = min(lo + each, count);
-  auto kinds = [&](int i, uint32_t* equal) {                   // which of a warp's 32 are taken anyway, and which agree
-    bool take = false, same = false;
-    if (i < hi) {
-      if (i < first || i >= end) {
-        take = true;
+  // Those above, and the first `left` of those that agree.  A warp notes for 32 neighbouring pages which are what, as bits; then a thread has 32 pages.
+  int* const list = kHeld ? reinterpret_cast<int*>(held_keys + p.width) : nullptr;
+  int2 front = make_int2(0, 0);                                // of the pages before these
+  for (int page0 = 0; page0 < count; page0 += 32 * kSelectThreads) {
+    const int pieces = min((count - page0 + 31) / 32, kSelectThreads);
+#pragma unroll 1
+    for (int c = wid; c < pieces; c += kSelectThreads / 32) {
+      const int i = page0 + 32 * c + lane;
+      const uint32_t k = i >= count ? 0u : i < first || i >= end ? 0xffffffffu : key(i) >> shift;      // (what is behind the last page may agree, and is not among the first)
+      const uint32_t take = __ballot_sync(0xffffffffu, k > prefix), same = __ballot_sync(0xffffffffu, k == prefix);
+      if (lane == 0) kinds[c] = make_uint2(take, same);
+    }
+    __syncthreads();
+    const uint2 mine = tid < pieces ? kinds[tid] : make_uint2(0, 0);
+    int2 n = make_int2(__popc(mine.x), __popc(mine.y));
+    const int2 own = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, n.x, o), y = __shfl_up_sync(0xffffffffu, n.y, o);
+      if (lane >= o) { n.x += x; n.y += y; }
+    }
+    if (lane == 31) totals[wid] = n;
+    __syncthreads();
+    const int2 all = lane < kSelectThreads / 32 ? totals[lane] : make_int2(0, 0);
+    int2 others = lane < wid ? all : make_int2(0, 0);          // of the warps in front
+#pragma unroll
+    for (int o = 16; o; o >>= 1) { others.x += __shfl_xor_sync(0xffffffffu, others.x, o); others.y += __shfl_xor_sync(0xffffffffu, others.y, o); }
+    n.x += front.x + others.x - own.x;
+    n.y += front.y + others.y - own.y;
+#pragma unroll 1
+    for (uint32_t bits = mine.x | (n.y < left ? mine.y : 0u); bits; bits &= bits - 1) {
+      const int at = __ffs(bits) - 1, same = n.y + __popc(mine.y & ((1u << at) - 1)), to = n.x + __popc(mine.x & ((1u << at) - 1)) + min(same, left);
+      const int page = page0 + 32 * tid + at;
+      if ((!(mine.x >> at & 1) && same >= left) || to >= p.keep) continue;      // (no more than `keep`, should the scores change meanwhile)
+      if (kHeld) {
+        list[to] = page;
       } else {
-        const uint32_t k = key(i) >> shift;
-        take = k > prefix;
-        same = k == prefix;
+        table[to] = entries[page];
+        if (chosen) chosen[to] = page;
       }
     }
-    *equal = __ballot_sync(0xffffffffu, same);
-    return __ballot_sync(0xffffffffu, take);
-  };
-  int2 n = make_int2(0, 0);
-  for (int i = lo; i < hi; i += 32) {
-    uint32_t equal;
-    n.x += __popc(kinds(i + lane, &equal));
-    n.y += __popc(equal);
-  }
-  if (lane == 0) totals[wid] = n;
-  __syncthreads();
-  n = lane < wid ? totals[lane] : make_int2(0, 0);             // in front of this warp's
-#pragma unroll
-  for (int o = 16; o; o >>= 1) { n.x += __shfl_xor_sync(0xffffffffu, n.x, o); n.y += __shfl_xor_sync(0xffffffffu, n.y, o); }
-  for (int i = lo; i < hi; i += 32) {
-    uint32_t equal;
-    const uint32_t take = kinds(i + lane, &equal), below = (1u << lane) - 1;
-    const int same = n.y + __popc(equal & below), to = n.x + __popc(take & below) + min(same, left);
-    if ((take >> lane & 1) || ((equal >> lane & 1) && same < left)) {
-      table[to] = entries[i + lane];
-      if (chosen) chosen[to] = i + lane;
+    if (page0 + 32 * kSelectThreads < count) {
+      front.x += __reduce_add_sync(0xffffffffu, all.x);
+      front.y += __reduce_add_sync(0xffffffffu, all.y);
     }
-    n.x += __popc(take);
-    n.y += __popc(equal);
+    __syncthreads();
+  }
+  if (kHeld) {
+    for (int i = tid; i < p.keep; i += kSelectThreads) {
+      table[i] = entries[list[i]];
+      if (chosen) chosen[i] = list[i];
+    }
   }
 }
 
@@ -490,13 +508,22 @@ cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t strea
   return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, blocks);
 }
 
-cudaError_t launch_pages_select(const SelectParams& p, cudaStream_t stream) {
+namespace {
+
+template <int kSelectThreads>
+cudaError_t launch_select(const SelectParams& p, cudaStream_t stream) {
   static std::atomic<uint64_t> done{0};
-  const dim3 grid(p.B * p.Sq);
-  if (p.width > kHeldKeys) return launch_in_order(pages_select_kernel<false>, grid, kSelectThreads, 0, stream, p);
-  const cudaError_t err = allow_shared(pages_select_kernel<true>, done, kHeldKeys * sizeof(uint32_t));
+  const cudaError_t err = allow_shared(pages_select_kernel<kSelectThreads, true>, done, 2 * kHeldPages * sizeof(uint32_t));
   if (err != cudaSuccess) return err;
-  return launch_in_order(pages_select_kernel<true>, grid, kSelectThreads, p.width <= p.keep ? 0 : p.width * static_cast<uint32_t>(sizeof(uint32_t)), stream, p);
+  return launch_in_order(pages_select_kernel<kSelectThreads, true>, dim3(p.B * p.Sq), kSelectThreads, p.width <= p.keep ? 0 : (p.width + p.keep) * static_cast<uint32_t>(sizeof(uint32_t)),
+                         stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_pages_select(const SelectParams& p, cudaStream_t stream) {
+  if (p.width > kHeldPages) return launch_in_order(pages_select_kernel<1024, false>, dim3(p.B * p.Sq), 1024, 0, stream, p);
+  return p.width <= 2048 ? launch_select<256>(p, stream) : launch_select<1024>(p, stream);
 }
 
 }  // namespace amla
