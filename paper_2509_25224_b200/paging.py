@@ -171,22 +171,13 @@ def _batch(cache, starts, block_table, seqlens):
     if on < 0:
         raise ValueError("paging works on CUDA tensors, not tensors on " + str(cache.device))
     fmt = cache_format(cache)
-    if not cache.is_contiguous():
-        raise ValueError("the cache must be contiguous")
-    _int32(starts, on, "starts")
-    _int32(block_table, on, "block_table")
-    _int32(seqlens, on, "seqlens")
-    if block_table.dim() != 2 or starts.dim() != 1 or seqlens.dim() != 1 or starts.numel() != block_table.shape[0] + 1 or seqlens.numel() != block_table.shape[0]:
+    if not (cache.is_contiguous() and starts.dtype is _int and starts.is_contiguous() and starts.get_device() == on and block_table.dtype is _int and block_table.is_contiguous()
+            and block_table.get_device() == on and seqlens.dtype is _int and seqlens.is_contiguous() and seqlens.get_device() == on):
+        raise ValueError("the cache must be contiguous, and starts, block_table and seqlens contiguous int32 tensors on its device")
+    shape = block_table.shape
+    if len(shape) != 2 or starts.dim() != 1 or seqlens.dim() != 1 or starts.numel() != shape[0] + 1 or seqlens.numel() != shape[0]:
         raise ValueError("block_table is [B, max_blocks], seqlens [B], starts [B + 1]")
-    B, width = block_table.shape
-    return on, fmt, B, width, cache.shape[0]
-
-
-def _steps(t, on, columns, name):
-    """Strides (in elements) of a bf16 tensor [..., columns] whose columns are contiguous; an axis of at most one entry has none that matters."""
-    if t.dtype is not _torch.bfloat16 or t.get_device() != on or t.shape[-1] != columns or (t.numel() > 0 and t.stride(-1) != 1):
-        raise ValueError("%s must be bfloat16 [..., %d] with contiguous columns on the device of the cache" % (name, columns))
-    return [step if n > 1 else columns for step, n in zip(t.stride()[:-1], t.shape)]
+    return on, fmt, shape[0], shape[1], cache.shape[0]
 
 
 def cache_append(kv, starts, cache, kv_scale: float, block_table, seqlens, cos_sin, positions=None, norm_weight=None, eps: float = 1e-6, interleaved: bool = False, q_pe=None, q=None) -> None:
@@ -199,39 +190,45 @@ def cache_append(kv, starts, cache, kv_scale: float, block_table, seqlens, cos_s
     is rotated into columns 512 .. 575 of q (bf16 [n, H, 576]).  ``include/amla.h`` says what happens to tokens without a place or a position."""
     L = _ready()
     on, fmt, B, width, blocks = _batch(cache, starts, block_table, seqlens)
-    if kv.dim() != 2:
-        raise ValueError("tokens are bfloat16 [n, 576]")
-    step, = _steps(kv, on, 576, "kv")
-    n = kv.shape[0]
-    if step < 576:
-        raise ValueError("rows of tokens must not overlap")
+    bf16 = _torch.bfloat16
+    shape = kv.shape
+    if kv.dtype is not bf16 or kv.get_device() != on or len(shape) != 2 or shape[1] != 576:
+        raise ValueError("tokens are bfloat16 [n, 576] on the device of the cache")
+    n = shape[0]
+    step, inner = kv.stride()
+    # (an axis of at most one entry has no stride that matters)
+    if n > 0 and (inner != 1 or (n > 1 and step < 576)):
+        raise ValueError("rows of tokens must have contiguous columns and not overlap")
     if cos_sin.dtype is not _torch.float32 or cos_sin.dim() != 2 or cos_sin.shape[1] != 64 or not cos_sin.is_contiguous() or cos_sin.get_device() != on:
         raise ValueError("cos_sin must be a contiguous float32 [n_positions, 64] on the device of the cache")
-    at = 0
+    at = weight = wide = H = from_q = from_token = from_head = to_q = to_token = to_head = 0
     if positions is not None:
         _int32(positions, on, "positions")
         if positions.dim() != 1 or positions.numel() != n:
             raise ValueError("positions is [n]")
         at = positions.data_ptr()
-    weight = wide = 0
     if norm_weight is not None:
-        wide = int(norm_weight.dtype is _torch.float32)
-        if not (wide or norm_weight.dtype is _torch.bfloat16) or norm_weight.shape != (512,) or not norm_weight.is_contiguous() or norm_weight.get_device() != on:
+        wide = 1 if norm_weight.dtype is _torch.float32 else 0
+        if not (wide or norm_weight.dtype is bf16) or norm_weight.dim() != 1 or norm_weight.numel() != 512 or not norm_weight.is_contiguous() or norm_weight.get_device() != on:
             raise ValueError("norm_weight must be a contiguous bfloat16 or float32 [512] on the device of the cache")
         weight = norm_weight.data_ptr()
-    if (q_pe is None) != (q is None):
-        raise ValueError("q_pe and q are given together, or neither")
-    from_q, to_q, H = (0, 0, 0), (0, 0, 0), 0
-    if q is not None:
-        if q_pe.dim() != 3 or q.dim() != 3 or q_pe.shape[:2] != q.shape[:2] or q.shape[0] != n:
+    if q is not None and q_pe is not None:
+        if q.dtype is not bf16 or q_pe.dtype is not bf16 or q.get_device() != on or q_pe.get_device() != on:
+            raise ValueError("q_pe and q must be bfloat16, on the device of the cache")
+        shape, source = q.shape, q_pe.shape
+        if len(shape) != 3 or len(source) != 3 or shape[0] != n or source[0] != n or source[1] != shape[1] or shape[2] != 576 or source[2] != 64:
             raise ValueError("q_pe is [n, H, 64] and q [n, H, 576]")
-        H = q.shape[1]
-        from_q, to_q = (q_pe.data_ptr(), *_steps(q_pe, on, 64, "q_pe")), (q.data_ptr(), *_steps(q, on, 576, "q"))
-        if min(to_q[1:]) < 576:
-            raise ValueError("rows of q must not overlap")
+        H = shape[1]
+        to_token, to_head, inner = q.stride()
+        from_token, from_head, columns = q_pe.stride()
+        if n > 0 and H > 0 and (inner != 1 or columns != 1 or (n > 1 and to_token < 576) or (H > 1 and to_head < 576)):
+            raise ValueError("rows of q and q_pe must have contiguous columns, and those of q must not overlap")
+        from_q, to_q = q_pe.data_ptr(), q.data_ptr()
+    elif q is not None or q_pe is not None:
+        raise ValueError("q_pe and q are given together, or neither")
     _call(on, L.amla_cache_append,
           (fmt, kv.data_ptr(), step, n, starts.data_ptr(), cache.data_ptr(), float(kv_scale), block_table.data_ptr(), seqlens.data_ptr(), B, blocks, width, cos_sin.data_ptr(),
-           cos_sin.shape[0], at, weight, wide, float(eps), int(interleaved), *from_q, *to_q, H), "amla_cache_append")
+           cos_sin.shape[0], at, weight, wide, float(eps), 1 if interleaved else 0, from_q, from_token, from_head, to_q, to_token, to_head, H), "amla_cache_append")
 
 
 def page_means(cache, kv_scale: float, block_table, seqlens, starts, n_tokens: int, means):

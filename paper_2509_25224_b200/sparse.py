@@ -48,9 +48,10 @@ def _queries(q, block_table, seqlens):
     paging._int32(block_table, on, "block_table")
     paging._int32(seqlens, on, "seqlens")
     B, Sq, H, _ = q.shape
-    if block_table.dim() != 2 or block_table.shape[0] != B or seqlens.shape != (B,):
+    shape = block_table.shape
+    if len(shape) != 2 or shape[0] != B or seqlens.dim() != 1 or seqlens.numel() != B:
         raise ValueError("block_table is [B, max_blocks], seqlens [B]")
-    return on, B, Sq, H, block_table.shape[1]
+    return on, B, Sq, H, shape[1]
 
 
 def _given(t, shape, dtype, on, like, name):
@@ -103,14 +104,14 @@ def pages_select(scores, block_table, seqlens, keep: int, sink: int = 1, recent:
     paging._int32(block_table, on, "block_table")
     paging._int32(seqlens, on, "seqlens")
     B, Sq, width = scores.shape
-    if block_table.shape != (B, width) or seqlens.shape != (B,):
+    if block_table.shape != (B, width) or seqlens.dim() != 1 or seqlens.numel() != B:
         raise ValueError("block_table is [B, max_blocks], seqlens [B]")
     keep = int(keep)
     if keep < 1:
         raise ValueError("keep is at least 1")
     table = _given(table, (B * Sq, keep), torch.int32, on, scores, "table")
-    lens = _given(lens, (B * Sq,), torch.int32, on, scores, "lens")
     chosen = _given(chosen, (B * Sq, keep), torch.int32, on, scores, "chosen")
+    lens = _given(lens, (B * Sq,), torch.int32, on, scores, "lens")
     paging._call(on, L.amla_pages_select,
                  (scores.data_ptr(), block_table.data_ptr(), seqlens.data_ptr(), B, Sq, width, keep, int(sink), int(recent), table.data_ptr(), lens.data_ptr(), chosen.data_ptr()),
                  "amla_pages_select")
