@@ -91,13 +91,12 @@ __device__ __forceinline__ uint32_t e4m3_byte_pair(float a, float b, float scale
 
 // N neighbouring columns of a key from `first` on, a group of 16 columns being 16 / N neighbouring lanes.
 template <int kFormat, int N>
-__device__ __forceinline__ void put(const AppendParams& p, Place at, int first, const float (&x)[N], bool there) {
+__device__ __forceinline__ void put(const AppendParams& p, Place at, int first, const float (&x)[N]) {
   if constexpr (kFormat == AMLA_CACHE_BF16) {
     __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.cache) + (at.page * kPage + at.row) * kDqk + first;
     uint32_t w[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) w[i] = sm100::pack_bf16x2(x[2 * i], x[2 * i + 1]);
-    if (!there) return;
     if constexpr (N == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
     else *reinterpret_cast<uint32_t*>(dst) = w[0];
   } else if constexpr (kFormat == AMLA_CACHE_E4M3) {
@@ -105,7 +104,6 @@ __device__ __forceinline__ void put(const AppendParams& p, Place at, int first, 
     uint32_t b[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) b[i] = e4m3_byte_pair(x[2 * i], x[2 * i + 1], p.kv_scale, p.inv_scale);
-    if (!there) return;
     if constexpr (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
     else *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(b[0]);
   } else {
@@ -122,7 +120,6 @@ __device__ __forceinline__ void put(const AppendParams& p, Place at, int first, 
     uint32_t codes = 0;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) codes |= e2m1_byte(quotient(x[2 * i], step, inv), quotient(x[2 * i + 1], step, inv)) << (8 * i);
-    if (!there) return;
     uint8_t* page = static_cast<uint8_t*>(p.cache) + at.page * kPageBytes4;
     uint8_t* dst = page + at.row * kCodeRow + first / 2;
     if constexpr (N == 8) *reinterpret_cast<uint32_t*>(dst) = codes;
@@ -131,16 +128,30 @@ __device__ __forceinline__ void put(const AppendParams& p, Place at, int first, 
   }
 }
 
-// A warp, a token.  A lane has columns 8 lane .. and 256 + 8 lane .. of the latent, and columns 2 lane, 2 lane + 1 of the position part,
+// A token's key as a lane has it: columns 8 lane .. and 256 + 8 lane .. of the latent, and columns 2 lane, 2 lane + 1 of the position part,
 // whose partners are its own (interleaved) or those of lane ^ 16.
-template <int kFormat, bool kWide, bool kInterleaved>
-__device__ __forceinline__ void append_token(const AppendParams& p, int token, Place at, int position, int lane) {
-  const bool there = at.page >= 0 && position >= 0;
-  if (!there) return;                                // (the whole warp)
+struct Key { uint4 latent[2]; float pe[2]; };
+
+template <bool kWide>
+__device__ __forceinline__ Key load_key(const AppendParams& p, int token, int lane) {
   const __nv_bfloat16* row = p.kv + token * p.row_stride;
-  const uint4 v0 = load8<kWide>(row + 8 * lane), v1 = load8<kWide>(row + kDv / 2 + 8 * lane);
   const unsigned short* tail = reinterpret_cast<const unsigned short*>(row + kDv + 2 * lane);
-  const float k0 = __uint_as_float(static_cast<uint32_t>(tail[0]) << 16), k1 = __uint_as_float(static_cast<uint32_t>(tail[1]) << 16);
+  Key k;
+  k.latent[0] = load8<kWide>(row + 8 * lane);
+  k.latent[1] = load8<kWide>(row + kDv / 2 + 8 * lane);
+  if (kWide) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(tail);
+    k.pe[0] = low(w);
+    k.pe[1] = high(w);
+  } else {
+    k.pe[0] = __uint_as_float(static_cast<uint32_t>(tail[0]) << 16);
+    k.pe[1] = __uint_as_float(static_cast<uint32_t>(tail[1]) << 16);
+  }
+  return k;
+}
+
+template <int kFormat, bool kWide, bool kInterleaved>
+__device__ __forceinline__ void store_key(const AppendParams& p, const Key& key, Place at, int position, int lane) {
   const float* angles = p.cos_sin + static_cast<size_t>(position) * kRope;
   float2 c, s;
   if (kInterleaved) {
@@ -151,8 +162,8 @@ __device__ __forceinline__ void append_token(const AppendParams& p, int token, P
     s = *reinterpret_cast<const float2*>(angles + kPairs + 2 * (lane & 15));
   }
   float x[2][8];
-  unpack8(v0, x[0]);
-  unpack8(v1, x[1]);
+  unpack8(key.latent[0], x[0]);
+  unpack8(key.latent[1], x[1]);
   if (p.weight) {
     float w[2][8];
 #pragma unroll
@@ -176,36 +187,55 @@ __device__ __forceinline__ void append_token(const AppendParams& p, int token, P
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const double mean = sum * (1. / kDv) + static_cast<double>(p.eps);
     const float m = static_cast<float>(mean);
-    const float r = m >= 0x1p-126f && m <= 0x1.fffffep127f ? rsqrtf(m) : static_cast<float>(rsqrt(mean));   // (squares may leave FP32's range where their root does not)
+    float r;
+    if (m >= 0x1p-126f && m <= 0x1.fffffep127f) {
+      r = rsqrtf(m);
+    } else {                                         // squares may leave FP32's range where their root does not
+      const bool small = mean < 1.;
+      r = rsqrtf(static_cast<float>(mean * (small ? 0x1p160 : 0x1p-160))) * (small ? 0x1p80f : 0x1p-80f);
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i >> 3][i & 7] = __fmul_rn(__fmul_rn(x[i >> 3][i & 7], r), w[i >> 3][i & 7]);
   }
   float y[2];
   if (kInterleaved) {
-    y[0] = turn_first(k0, k1, c.x, s.x);
-    y[1] = turn_second(k0, k1, c.x, s.x);
+    y[0] = turn_first(key.pe[0], key.pe[1], c.x, s.x);
+    y[1] = turn_second(key.pe[0], key.pe[1], c.x, s.x);
   } else {
-    const float o0 = __shfl_xor_sync(0xffffffffu, k0, 16), o1 = __shfl_xor_sync(0xffffffffu, k1, 16);
-    y[0] = lane < 16 ? turn_first(k0, o0, c.x, s.x) : turn_second(o0, k0, c.x, s.x);
-    y[1] = lane < 16 ? turn_first(k1, o1, c.y, s.y) : turn_second(o1, k1, c.y, s.y);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float other = __shfl_xor_sync(0xffffffffu, key.pe[i], 16), cc = i ? c.y : c.x, ss = i ? s.y : s.x;
+      y[i] = lane < 16 ? turn_first(key.pe[i], other, cc, ss) : turn_second(other, key.pe[i], cc, ss);
+    }
   }
-  put<kFormat, 8>(p, at, 8 * lane, x[0], there);
-  put<kFormat, 8>(p, at, kDv / 2 + 8 * lane, x[1], there);
-  put<kFormat, 2>(p, at, kDv + 2 * lane, y, there);
+  put<kFormat, 8>(p, at, 8 * lane, x[0]);
+  put<kFormat, 8>(p, at, kDv / 2 + 8 * lane, x[1]);
+  put<kFormat, 2>(p, at, kDv + 2 * lane, y);
 }
 
-// A query's 64 columns by eight lanes: lane i of them has columns 8 i .., whose partners are its own (interleaved) or those of lane i ^ 4.
-template <bool kWide, bool kInterleaved>
-__device__ __forceinline__ uint4 rotate8(uint4 v, const float* angles, int i) {
+// The angles of a query's eight columns 8 i .., whose partners are their own neighbours (interleaved) or those of lane i ^ 4.
+template <bool kInterleaved>
+struct Angles {
+  static constexpr int kCount = kInterleaved ? 4 : 8;
+  float c[kCount], s[kCount];
+  __device__ __forceinline__ Angles(const float* row, int i) {
+    const float* a = row + (kInterleaved ? 4 * i : 8 * (i & 3));
+#pragma unroll
+    for (int k = 0; k < kCount; k += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(a + k), y = *reinterpret_cast<const float4*>(a + kPairs + k);
+      c[k] = x.x; c[k + 1] = x.y; c[k + 2] = x.z; c[k + 3] = x.w;
+      s[k] = y.x; s[k + 1] = y.y; s[k + 2] = y.z; s[k + 3] = y.w;
+    }
+  }
+};
+template <bool kInterleaved>
+__device__ __forceinline__ uint4 rotate8(uint4 v, const Angles<kInterleaved>& a, int i) {
   float x[8], y[8];
   unpack8(v, x);
-  if (kInterleaved) {
-    const float4 c = *reinterpret_cast<const float4*>(angles + 4 * i), s = *reinterpret_cast<const float4*>(angles + kPairs + 4 * i);
-    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+  if constexpr (kInterleaved) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { y[2 * k] = turn_first(x[2 * k], x[2 * k + 1], cc[k], ss[k]); y[2 * k + 1] = turn_second(x[2 * k], x[2 * k + 1], cc[k], ss[k]); }
+    for (int k = 0; k < 4; ++k) { y[2 * k] = turn_first(x[2 * k], x[2 * k + 1], a.c[k], a.s[k]); y[2 * k + 1] = turn_second(x[2 * k], x[2 * k + 1], a.c[k], a.s[k]); }
   } else {
-    const float* a = angles + 8 * (i & 3);
     uint4 other;
     other.x = __shfl_xor_sync(0xffffffffu, v.x, 4);
     other.y = __shfl_xor_sync(0xffffffffu, v.y, 4);
@@ -214,46 +244,43 @@ __device__ __forceinline__ uint4 rotate8(uint4 v, const float* angles, int i) {
     float z[8];
     unpack8(other, z);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float4 c = reinterpret_cast<const float4*>(a)[h], s = reinterpret_cast<const float4*>(a + kPairs)[h];
-      const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) y[4 * h + k] = i < 4 ? turn_first(x[4 * h + k], z[4 * h + k], cc[k], ss[k]) : turn_second(z[4 * h + k], x[4 * h + k], cc[k], ss[k]);
-    }
+    for (int k = 0; k < 8; ++k) y[k] = i < 4 ? turn_first(x[k], z[k], a.c[k], a.s[k]) : turn_second(z[k], x[k], a.c[k], a.s[k]);
   }
   return make_uint4(sm100::pack_bf16x2(y[0], y[1]), sm100::pack_bf16x2(y[2], y[3]), sm100::pack_bf16x2(y[4], y[5]), sm100::pack_bf16x2(y[6], y[7]));
 }
 
+constexpr int kWarpHeads = 16, kRounds = kWarpHeads / 4;      // queries of a warp: four at a time, eight lanes each
+
 }  // namespace
 
-// A block has kTokens tokens: a warp finds a token's place and writes its key; then all warps rotate the tokens' queries.
-template <int kFormat, bool kWide, bool kInterleaved, int kTokens>
-__global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p) {
-  __shared__ int position_of[kTokens];
+// A warp: up to sixteen of a token's queries and, the token's first warp, its key.  What it reads of the token is on its way before it looks for the
+// token's place; it finds that by itself, so that no warp waits for another.
+template <int kFormat, bool kWide, bool kInterleaved>
+__global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p, int warps_of_token) {
   behind_the_kernel_in_front();
-  const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31, token0 = blockIdx.x * kTokens;
-  for (int i = wid; i < kTokens; i += kWarps) {
-    const int token = token0 + i;
-    int position = -1;
-    if (token < p.tokens.n) {
-      const Place at = place_of_token(p.tokens, token, lane);
-      position = p.positions ? p.positions[token] : at.position;
-      if (position >= p.n_positions) position = -1;
-      append_token<kFormat, kWide, kInterleaved>(p, token, at, position, lane);
+  const int lane = threadIdx.x & 31;
+  const long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int token = static_cast<int>(unit / warps_of_token), mine = static_cast<int>(unit % warps_of_token);
+  if (token >= p.tokens.n) return;
+  const int i = lane & 7, head = mine * kWarpHeads + (lane >> 3);
+  uint4 v[kRounds];
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k)
+    v[k] = head + 4 * k < p.H ? load8<kWide>(p.q_pe + token * p.q_pe_token + (head + 4 * k) * p.q_pe_head + 8 * i) : make_uint4(0, 0, 0, 0);
+  Key key;
+  if (mine == 0) key = load_key<kWide>(p, token, lane);
+  const Place at = place_of_token(p.tokens, token, lane);
+  const int position = p.positions ? p.positions[token] : at.position;
+  if (position < 0 || position >= p.n_positions) return;
+  if (mine * kWarpHeads < p.H) {
+    const Angles<kInterleaved> angles(p.cos_sin + static_cast<size_t>(position) * kRope, i);
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      const uint4 y = rotate8<kInterleaved>(v[k], angles, i);
+      if (head + 4 * k < p.H) store8<kWide>(p.q + token * p.q_token + (head + 4 * k) * p.q_head + kDv + 8 * i, y);
     }
-    if (lane == 0) position_of[i] = position;
   }
-  if (p.H == 0) return;
-  __syncthreads();
-  const int items = kTokens * p.H * 8;
-  for (int k = threadIdx.x; k < (items + 31) / 32 * 32; k += kThreads) {      // (whole warps)
-    const int i = k & 7, row = k >> 3, mine = min(row / p.H, kTokens - 1), head = row % p.H, token = token0 + mine;
-    const int position = k < items ? position_of[mine] : -1;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (position >= 0) v = load8<kWide>(p.q_pe + token * p.q_pe_token + head * p.q_pe_head + 8 * i);
-    const uint4 y = rotate8<kWide, kInterleaved>(v, p.cos_sin + static_cast<size_t>(max(position, 0)) * kRope, i);
-    if (position >= 0) store8<kWide>(p.q + token * p.q_token + head * p.q_head + kDv + 8 * i, y);
-  }
+  if (mine == 0 && at.page >= 0) store_key<kFormat, kWide, kInterleaved>(p, key, at, position, lane);
 }
 
 namespace {
@@ -354,8 +381,9 @@ int check_books(const int32_t* starts, const void* cache, const int32_t* block_t
 
 template <int kFormat, bool kWide, bool kInterleaved>
 cudaError_t launch_append(const AppendParams& p, cudaStream_t stream) {
-  if (p.H > 32) return launch_in_order(append_kernel<kFormat, kWide, kInterleaved, 1>, dim3(p.tokens.n), kThreads, 0, stream, p);
-  return launch_in_order(append_kernel<kFormat, kWide, kInterleaved, kWarps>, dim3((p.tokens.n + kWarps - 1) / kWarps), kThreads, 0, stream, p);
+  const int warps = p.H > kWarpHeads ? (p.H + kWarpHeads - 1) / kWarpHeads : 1;
+  const long long blocks = (static_cast<long long>(p.tokens.n) * warps + kWarps - 1) / kWarps;
+  return launch_in_order(append_kernel<kFormat, kWide, kInterleaved>, dim3(static_cast<unsigned>(blocks)), kThreads, 0, stream, p, warps);
 }
 template <int kFormat>
 cudaError_t launch_append(const AppendParams& p, bool wide, bool interleaved, cudaStream_t stream) {
@@ -382,7 +410,7 @@ extern "C" int amla_cache_append(int format, const void* kv, long long row_strid
   if (H > 0) {
     if (!q_pe || !q || !aligned(q_pe, 2) || !aligned(q, 2) || q_pe_token_stride < 0 || q_pe_head_stride < 0) return AMLA_ERR_INVALID_ARG;
     if ((n_tokens > 1 && q_token_stride < kDqk) || (H > 1 && q_head_stride < kDqk)) return AMLA_ERR_INVALID_ARG;
-    if (H > 1024) return AMLA_ERR_UNSUPPORTED;
+    if (H > 1024 || static_cast<long long>(n_tokens) * H > (1ll << 34)) return AMLA_ERR_UNSUPPORTED;      // (blocks of a grid)
   }
   AppendParams p = {};
   p.kv = static_cast<const __nv_bfloat16*>(kv);

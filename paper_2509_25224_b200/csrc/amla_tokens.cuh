@@ -28,21 +28,26 @@ __device__ __forceinline__ void behind_the_kernel_in_front() {
 }
 
 // By a whole warp, which gets the same answer in every lane.  The sequence is the last one that begins at or before the token (one without
-// tokens holds none): 32 candidates at a time, so that up to 1024 sequences take two dependent reads.
+// tokens holds none): 32 candidates at a time, the last 32 with their ends and lengths, so that up to 32 sequences take two dependent reads
+// (the other is the page number), up to 1024 three.
 __device__ __forceinline__ Place place_of_token(const Tokens& t, int token, int lane) {
   Place p{-1, 0, -1};
   int lo = 0, n = t.B;
-  while (n > 1) {
+  while (n > 32) {
     const int step = (n + 31) / 32, at = lane * step;
-    const bool before = at < n && t.starts[lo + at] <= token;
-    const uint32_t yes = __ballot_sync(0xffffffffu, before);
+    const uint32_t yes = __ballot_sync(0xffffffffu, at < n && t.starts[lo + at] <= token);
     const int last = yes ? 31 - __clz(yes) : 0;
     lo += last * step;
     n = min(step, n - last * step);
   }
-  const int begin = t.starts[lo], end = t.starts[lo + 1];
+  const int start = t.starts[lo + min(lane, n)], len = t.seqlens[lo + min(lane, n - 1)];
+  const uint32_t yes = __ballot_sync(0xffffffffu, lane < n && start <= token);
+  const int last = yes ? 31 - __clz(yes) : 0;
+  const int begin = __shfl_sync(0xffffffffu, start, last), next = __shfl_sync(0xffffffffu, start, min(last + 1, 31)), keys = __shfl_sync(0xffffffffu, len, last);
+  const int end = last < 31 ? next : t.starts[lo + 32];
+  lo += last;
   if (token < begin || token >= end) return p;
-  const long long at = static_cast<long long>(t.seqlens[lo]) - (end - token);
+  const long long at = static_cast<long long>(keys) - (end - token);
   if (at < 0) return p;
   p.position = static_cast<int>(at);
   p.row = static_cast<int>(at % kPage);
