@@ -291,13 +291,13 @@ int amla_page_means(int format, const void* kv_cache, float kv_scale, const int3
  *         holds a NaN or an infinity makes its token's scores NaN.
  * select: of the pages that a token sees, the first `sink`, the last `recent` (at least 1) and, of the others, those with the largest scores,
  *         `keep` in all (sink + recent <= keep); where scores are equal the lower position comes first, and a NaN counts as -infinity.
- *         Scores of other pages are not read.  For row r = b * Sq + t: table[r] (int32 [B * Sq, keep]) has the pages' entries of the block
+ *         Scores of other pages do not matter.  For row r = b * Sq + t: table[r] (int32 [B * Sq, keep]) has the pages' entries of the block
  *         table in order of position, lens[r] (int32 [B * Sq]) the number of keys in them (all but the last page are full), chosen[r] (int32 [B * Sq, keep], or NULL) their
- *         positions in block_table[b]; -1 beyond.  table and lens are a block table and lengths for any of the decode
+ *         positions in block_table[b]; -1 beyond.  The three must not overlap the inputs, nor one another.  table and lens are a block table and lengths for any of the decode
  *         calls on B * Sq sequences of one query token each (q [B, Sq, H, 576] as it lies).
- * decode: all of it: scores, selection, attention.  lse is that of the keys attended to.  Where max_blocks_per_seq <= keep no page is left out, means is not
- *         read (and may be NULL), and the result is that of the plain call.
- * workspace: 256-byte aligned, at least as many bytes as the size function says; 1 <= Sq <= 8, 1 <= H <= 128, B * max_blocks_per_seq <= 2^28.  The status is read with
+ * decode: all of it: scores, selection, attention.  lse is that of the keys attended to.  Where max_blocks_per_seq <= keep no page is left out and means is not
+ *         read (and may be NULL).
+ * A length beyond the table counts as its width.  workspace: 256-byte aligned, at least as many bytes as the size function says (calls that overlap in time need distinct ones); 1 <= Sq <= 8, 1 <= H <= 128, B * max_blocks_per_seq <= 2^28, B * Sq <= 2^23.  The status is read with
  * amla_check_status for scores and amla_sparse_check_status for decode.
  */
 int amla_page_scores_workspace_size(int B, int Sq, int H, int max_blocks_per_seq, int device, size_t* bytes_out);

@@ -474,6 +474,15 @@ int check_selection(const int32_t* block_table, const int32_t* seqlens, int keep
   return AMLA_OK;
 }
 
+struct Extent {
+  const void* p;
+  size_t bytes;
+  bool meets(const Extent& o) const {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+    return bytes > 0 && o.bytes > 0 && a < b + o.bytes && b < a + bytes;
+  }
+};
+
 int device_of_call(int* device, int* sms) {
   if (cudaGetDevice(device) != cudaSuccess) { cudaGetLastError(); return AMLA_ERR_CUDA; }
   int cc = 0;
@@ -520,6 +529,14 @@ extern "C" int amla_pages_select(const float* scores, const int32_t* block_table
   if (rc != AMLA_OK) return rc;
   if ((!scores && max_blocks_per_seq > keep) || !table || !lens) return AMLA_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(scores) | reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(chosen)) & 3) return AMLA_ERR_INVALID_ARG;
+  // a row's answer must not be another row's question, nor two answers one
+  const size_t tokens = static_cast<size_t>(B) * Sq, entries = static_cast<size_t>(B) * max_blocks_per_seq;
+  const Extent in[3] = {{block_table, entries * 4}, {seqlens, static_cast<size_t>(B) * 4}, {scores, scores ? entries * Sq * 4 : 0}};
+  const Extent result[3] = {{table, tokens * keep * 4}, {lens, tokens * 4}, {chosen, chosen ? tokens * keep * 4 : 0}};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 3; ++j)
+      if (result[i].meets(in[j]) || (i < j && result[i].meets(result[j]))) return AMLA_ERR_INVALID_ARG;
+  }
   return launched(launch_pages_select(SelectParams{scores, block_table, seqlens, B, Sq, max_blocks_per_seq, keep, sink, recent, table, lens, chosen, nullptr},
                                       static_cast<cudaStream_t>(cuda_stream)));
 }

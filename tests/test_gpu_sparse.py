@@ -182,7 +182,7 @@ def test_selection_of_long_contexts(W, keep):
     check_select(np.exp(3 * rng.standard_normal((2, 1, W))), [64 * W - 30, 64 * (W - 1)], keep, 0, 1)
 
 
-def test_selection_reads_no_score_of_other_pages():
+def test_selection_goes_by_no_score_of_other_pages():
     s = np.random.default_rng(1).random((1, 1, 50))
     poisoned = s.copy()
     poisoned[..., :2], poisoned[..., 37:] = np.nan, np.inf
