@@ -256,12 +256,12 @@ constexpr int kWarpHeads = 16, kRounds = kWarpHeads / 4;      // queries of a wa
 // A warp: up to sixteen of a token's queries and, the token's first warp, its key.  What it reads of the token is on its way before it looks for the
 // token's place; it finds that by itself, so that no warp waits for another.
 template <int kFormat, bool kWide, bool kInterleaved>
-__global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p, int warps_of_token) {
+__global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p, uint32_t warps_of_token) {
   behind_the_kernel_in_front();
   const int lane = threadIdx.x & 31;
-  const long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  const int token = static_cast<int>(unit / warps_of_token), mine = static_cast<int>(unit % warps_of_token);
-  if (token >= p.tokens.n) return;
+  const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if (unit / warps_of_token >= static_cast<uint32_t>(p.tokens.n)) return;
+  const int token = unit / warps_of_token, mine = unit % warps_of_token;
   const int i = lane & 7, head = mine * kWarpHeads + (lane >> 3);
   uint4 v[kRounds];
 #pragma unroll
@@ -381,9 +381,8 @@ int check_books(const int32_t* starts, const void* cache, const int32_t* block_t
 
 template <int kFormat, bool kWide, bool kInterleaved>
 cudaError_t launch_append(const AppendParams& p, cudaStream_t stream) {
-  const int warps = p.H > kWarpHeads ? (p.H + kWarpHeads - 1) / kWarpHeads : 1;
-  const long long blocks = (static_cast<long long>(p.tokens.n) * warps + kWarps - 1) / kWarps;
-  return launch_in_order(append_kernel<kFormat, kWide, kInterleaved>, dim3(static_cast<unsigned>(blocks)), kThreads, 0, stream, p, warps);
+  const uint32_t warps = p.H > kWarpHeads ? (p.H + kWarpHeads - 1) / kWarpHeads : 1;
+  return launch_in_order(append_kernel<kFormat, kWide, kInterleaved>, dim3((p.tokens.n * warps + kWarps - 1) / kWarps), kThreads, 0, stream, p, warps);
 }
 template <int kFormat>
 cudaError_t launch_append(const AppendParams& p, bool wide, bool interleaved, cudaStream_t stream) {
@@ -410,7 +409,7 @@ extern "C" int amla_cache_append(int format, const void* kv, long long row_strid
   if (H > 0) {
     if (!q_pe || !q || !aligned(q_pe, 2) || !aligned(q, 2) || q_pe_token_stride < 0 || q_pe_head_stride < 0) return AMLA_ERR_INVALID_ARG;
     if ((n_tokens > 1 && q_token_stride < kDqk) || (H > 1 && q_head_stride < kDqk)) return AMLA_ERR_INVALID_ARG;
-    if (H > 1024 || static_cast<long long>(n_tokens) * H > (1ll << 34)) return AMLA_ERR_UNSUPPORTED;      // (blocks of a grid)
+    if (H > 1024 || static_cast<long long>(n_tokens) * H > (1ll << 34)) return AMLA_ERR_UNSUPPORTED;      // (warps are counted in 32 bits)
   }
   AppendParams p = {};
   p.kv = static_cast<const __nv_bfloat16*>(kv);
