@@ -1,4 +1,18 @@
 // Which pages of a long context a query token attends to: scores from the pages' means, and the choice.
+//
+// scores: l[h,p] = scale q_h . mean_p (products of bf16 on the tensor cores, FP32 sums), score[p] = sum_h 2^(l[h,p] - lse_h), lse_h over all pages p in front of the
+// token's own.  A head's lse needs all of its pages before any share of it is known: blocks of a cluster keep their logits in tensor memory until they have
+// exchanged a maximum and a sum for each row, so that every mean is read once and no logit is written.  (Logits by way of memory, two launches:
+// 32 x 65536 keys 23 us, 15.8 this way.  A sum of heads, not a maximum, because all heads attend to what is selected.)
+// What bounds it, 32 x 65536 keys of 128 heads, 15.8 us, 27 K clk a block: 2.5 K until the length is there; the first means 4.5 K later; then 37.7 MB of means at
+// 6.4 TB/s until 16.7 K; statistics 3.5 K, exchange 1.4 K, shares 2.9 K and their sums 1.9 K, all code that runs once.  Short contexts (8 x 1.5-4 K, 16 heads) take 6.5 us, a
+// launch and that chain; long ragged ones (12 x 9-262 K, two tokens, 27 us) wait for the longest sequence, of whose tiles half are multiplied twice.
+// One lane a scheduler is all that a loading warp gets, so that every address is at hand before the loop (1200 -> 350 clk for an operand place of a short context).
+// Tried: Q kept in shared memory beside a ring of 64 KB (three quarters of the bytes under way: 16.4 us, 45.7 for the long ragged ones); 16 summing warps (16.1); shares of the last
+// tile kept from the first pass over its logits (15.3, but 28.8 for the long ragged ones).
+//
+// select: a block for a query token.  4.5 us for 512 pages, 10.3 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
+// runs once, which rolled loops of 256 threads do in less time than unrolled ones of 1024 (up to 2048 pages; 16 K pages take 1024 threads 10.3 us).
 #include "../../include/amla.h"
 #include "amla_fp4.cuh"
 #include "amla_host.cuh"
@@ -486,8 +500,10 @@ int clusters_of_16() {
   return k.load(std::memory_order_acquire) - 1;
 }
 
-// Blocks in a cluster: as many as there are SMs for, but none that would have less than 64 pages of the longest sequence, and sixteen only where
-// that leaves no block with more than a tile, or fewer tiles, and all clusters have room.
+// Blocks in a cluster: as many as there are SMs for, but none that would have less than 64 pages of the longest sequence, and sixteen only where blocks of eight
+// would have more than a tile and all clusters have room at once.  Measured (blocks 1 / 2 / 4 / 8 / 16, us): 32 x 65536 keys 38.3 / 20.7 / 15.7 / 31.2; 128 x 16384 17.9 / 23.8 /
+// 36.6 / 77.3; 64 x 1-65 K 38.5 / 21.2 / 25.6 / 45.5; 16 x 65536 of two tokens 35.4 / 18.4 / 12.9 / 28.1; 1 x 262144 100 / 52 / 28 / 14.4 / 10.8; 8 x 262144, of
+// whose clusters of sixteen seven have room, - / - / - / 20.6 / 27.8.
 int score_blocks(int items, int width, int sms) {
   int blocks = 1;
   while (blocks < 8 && static_cast<long long>(items) * 2 * blocks <= sms && width > 64 * blocks) blocks *= 2;

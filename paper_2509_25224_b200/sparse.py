@@ -109,9 +109,10 @@ def pages_select(scores, block_table, seqlens, keep: int, sink: int = 1, recent:
     keep = int(keep)
     if keep < 1:
         raise ValueError("keep is at least 1")
-    table = _given(table, (B * Sq, keep), torch.int32, on, scores, "table")
-    chosen = _given(chosen, (B * Sq, keep), torch.int32, on, scores, "chosen")
-    lens = _given(lens, (B * Sq,), torch.int32, on, scores, "lens")
+    n, int32 = B * Sq, torch.int32
+    table = block_table.new_empty(n, keep) if table is None else _given(table, (n, keep), int32, on, scores, "table")
+    lens = block_table.new_empty(n) if lens is None else _given(lens, (n,), int32, on, scores, "lens")
+    chosen = block_table.new_empty(n, keep) if chosen is None else _given(chosen, (n, keep), int32, on, scores, "chosen")
     paging._call(on, L.amla_pages_select,
                  (scores.data_ptr(), block_table.data_ptr(), seqlens.data_ptr(), B, Sq, width, keep, int(sink), int(recent), table.data_ptr(), lens.data_ptr(), chosen.data_ptr()),
                  "amla_pages_select")

@@ -163,8 +163,8 @@ class Standin:
     def element_size(self):
         return 1
 
-    def new_empty(self, shape, dtype=None):
-        return Standin((shape,) if isinstance(shape, int) else shape, self.dtype if dtype is None else dtype, self._on)
+    def new_empty(self, *shape, dtype=None):
+        return Standin(shape[0] if isinstance(shape[0], tuple) else shape, self.dtype if dtype is None else dtype, self._on)
 
 
 B16, I32, U8, F32 = torch.bfloat16, torch.int32, torch.uint8, torch.float32
