@@ -287,7 +287,7 @@ int amla_page_means(int format, const void* kv_cache, float kv_scale, const int3
  *
  * scores: scores[b,t,p] = sum_h softmax_p(softmax_scale * q[b,t,h,:] . means[page p of sequence b]) over the pages p in front of the one that holds
  *         the query token's own position, which are full; 0 elsewhere.  It is the heads' attention that a page would have, were all of its keys
- *         their mean.  scores: fp32 [B, Sq, max_blocks_per_seq], 16-byte aligned.  A table entry outside [0, num_blocks) counts as a mean of zeros.  A row of q that
+ *         their mean.  scores: fp32 [B, Sq, max_blocks_per_seq].  A table entry outside [0, num_blocks) counts as a mean of zeros.  A row of q that
  *         holds a NaN or an infinity, or a page in front whose mean does (one that has never been written, say), makes its token's scores NaN.
  * select: of the pages that a token sees, the first `sink`, the last `recent` (at least 1) and, of the others, those with the largest scores,
  *         `keep` in all (sink + recent <= keep); where scores are equal the lower position comes first, and a NaN counts as -infinity.

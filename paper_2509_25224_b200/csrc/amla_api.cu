@@ -508,7 +508,7 @@ extern "C" int amla_page_scores_workspace_size(int B, int Sq, int H, int max_blo
 
 extern "C" int amla_page_scores(const void* q, const void* means, const int32_t* block_table, const int32_t* seqlens, float softmax_scale, int B, int Sq, int H, int num_blocks,
                                 int max_blocks_per_seq, float* scores, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-  int rc = check_arguments(q, means, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks, max_blocks_per_seq, scores, scores, workspace, 0);
+  int rc = check_arguments(q, means, block_table, seqlens, softmax_scale, B, Sq, H, num_blocks, max_blocks_per_seq, q, scores, workspace, 0);
   if (rc != AMLA_OK) return rc;
   if (static_cast<long long>(B) * max_blocks_per_seq > kMostScored) return AMLA_ERR_UNSUPPORTED;
   if (workspace_bytes < kScoresBytes) return AMLA_ERR_WORKSPACE;

@@ -112,6 +112,22 @@ def test_scores_twice_are_the_same_bits():
         assert torch.equal(a, sparse.page_scores(q, means, table, lens, 0.1))
 
 
+def test_scores_and_answers_at_any_address():
+    """Views that begin at 4 bytes, with something in front and behind that stays as it was."""
+    table, blocks = scattered([1000, 900, 64 * 31])
+    lens, W, keep = dev(np.array([1000, 900, 64 * 31], np.int32)), table.shape[1], 5
+    table = dev(table)
+    q, means = torch.randn(3, 1, 40, 576, device="cuda").bfloat16(), torch.randn(blocks, 576, device="cuda").bfloat16()
+    want = sparse.page_scores(q, means, table, lens, SCALE)
+    room = torch.full((3 * W + 2,), 7.0, device="cuda")
+    got = sparse.page_scores(q, means, table, lens, SCALE, room[1:-1].view(3, 1, W))
+    assert torch.equal(got, want) and float(room[0]) == float(room[-1]) == 7.0
+    a, b, c = sparse.pages_select(want, table, lens, keep)
+    rooms = [torch.full((n + 2,), 77, dtype=torch.int32, device="cuda") for n in (3 * keep, 3, 3 * keep)]
+    x, y, z = sparse.pages_select(got, table, lens, keep, table=rooms[0][1:-1].view(3, keep), lens=rooms[1][1:-1], chosen=rooms[2][1:-1].view(3, keep))
+    assert torch.equal(a, x) and torch.equal(b, y) and torch.equal(c, z) and all(int(r[0]) == int(r[-1]) == 77 for r in rooms)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 def test_a_row_that_is_not_a_number_spoils_its_own_token_only(bad):
     table, blocks = scattered([1000, 900])
@@ -124,6 +140,17 @@ def test_a_row_that_is_not_a_number_spoils_its_own_token_only(bad):
     same = [(0, 0), (0, 1), (1, 1)]
     assert all(torch.equal(got[i], good[i]) for i in same)
     assert torch.isnan(got[1, 0, :14]).all() and not got[1, 0, 14:].any()
+
+
+def test_a_mean_that_is_not_a_number_spoils_the_tokens_that_have_it_in_front():
+    table, blocks = scattered([1000, 900])
+    q, means = torch.randn(2, 2, 16, 576, device="cuda").bfloat16(), torch.randn(blocks, 576, device="cuda").bfloat16()
+    args = (q, means, dev(table), dev(np.array([1000, 900], np.int32)), SCALE)
+    good = sparse.page_scores(*args)
+    means[int(table[0, 15])] = float("nan")              # the page of the first sequence's last tokens: not scored
+    means[int(table[1, 3]), 5] = float("inf")
+    got = sparse.page_scores(*args)
+    assert torch.equal(got[0], good[0]) and torch.isnan(got[1, :, :14]).all() and not got[1, :, 14:].any()
 
 
 def test_the_wait_status_is_reset():

@@ -63,7 +63,7 @@ def scores(lib, q=at(0), m=at(0), table=at(0), lens=at(0), scale=0.1, B=1, Sq=1,
     return lib.amla_page_scores(q, m, table, lens, scale, B, Sq, H, blocks, width, out, ws, size, Z)
 
 
-@pytest.mark.parametrize("bad", [dict(q=Z), dict(m=Z), dict(table=Z), dict(lens=Z), dict(out=Z), dict(ws=Z), dict(q=at(8)), dict(m=at(8)), dict(out=at(8)), dict(table=at(2)), dict(lens=at(2)), dict(ws=at(16)),
+@pytest.mark.parametrize("bad", [dict(q=Z), dict(m=Z), dict(table=Z), dict(lens=Z), dict(out=Z), dict(ws=Z), dict(q=at(8)), dict(m=at(8)), dict(out=at(2)), dict(table=at(2)), dict(lens=at(2)), dict(ws=at(16)),
                                  dict(B=0), dict(Sq=0), dict(H=0), dict(blocks=0), dict(width=0), dict(scale=math.nan)])
 def test_scores_refuse(lib, bad):
     assert scores(lib, **bad) == BAD
