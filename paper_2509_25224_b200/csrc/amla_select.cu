@@ -3,16 +3,18 @@
 // scores: l[h,p] = scale q_h . mean_p (products of bf16 on the tensor cores, FP32 sums), score[p] = sum_h 2^(l[h,p] - lse_h), lse_h over all pages p in front of the
 // token's own.  A head's lse needs all of its pages before any share of it is known: blocks of a cluster keep their logits in tensor memory until they have
 // exchanged a maximum and a sum for each row, so that every mean is read once and no logit is written.  (Logits by way of memory, two launches:
-// 32 x 65536 keys 23 us, 15.8 this way.  A sum of heads, not a maximum, because all heads attend to what is selected.)
-// What bounds it, 32 x 65536 keys of 128 heads, 15.8 us, 27 K clk a block: 2.5 K until the length is there; the first means 4.5 K later; then 37.7 MB of means at
-// 6.4 TB/s until 16.7 K; statistics 3.5 K, exchange 1.4 K, shares 2.9 K and their sums 1.9 K, all code that runs once.  Short contexts (8 x 1.5-4 K, 16 heads) take 6.5 us, a
-// launch and that chain; long ragged ones (12 x 9-262 K, two tokens, 27 us) wait for the longest sequence, of whose tiles half are multiplied twice.
+// 32 x 65536 keys 23 us, 15.5 this way.  A sum of heads, not a maximum, because all heads attend to what is selected.)
+// What bounds it, 32 x 65536 keys of 128 heads, 15.5 us, 26 K clk a block: 2.5 K until the length is there; the first means 4.5 K later; then 37.7 MB of means at
+// 6.4 TB/s until 16.5 K; statistics 2.8 K and shares 2.9 K (2 K each are exponentials, sixteen a clock), exchange 1.4 K, sums 1.9 K.  Short contexts (8 x 1.5-4 K, 16 heads) take 6.5 us, a
+// launch and that chain; long ragged ones (12 x 9-262 K, two tokens, 26.9 us) wait for the longest sequence, of whose tiles half are multiplied twice.
 // One lane a scheduler is all that a loading warp gets, so that every address is at hand before the loop (1200 -> 350 clk for an operand place of a short context).
-// Tried: Q kept in shared memory beside a ring of 64 KB (three quarters of the bytes under way: 16.4 us, 45.7 for the long ragged ones); 16 summing warps (16.1); shares of the last
-// tile kept from the first pass over its logits (15.3, but 28.8 for the long ragged ones).
+// Tried: Q kept in shared memory beside a ring of 64 KB (a third of the bytes under way: 16.4 us, 45.7 for the long ragged ones); 16 summing warps (16.1); shares of the last
+// tile kept from the first pass over its logits (0.5 less, 1.5 more for the long ragged ones).
 //
 // select: a block for a query token.  4.5 us for 512 pages, 10.3 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
 // runs once, which rolled loops of 256 threads do in less time than unrolled ones of 1024 (up to 2048 pages; 16 K pages take 1024 threads 10.3 us).
+#include <type_traits>
+
 #include "../../include/amla.h"
 #include "amla_fp4.cuh"
 #include "amla_host.cuh"
@@ -179,6 +181,10 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
       tmem_ld_32x32b_x32(at + 32, v[1]);
       tmem_wait_ld();
     };
+    // (a comparison and a choice for every logit take as long as half of its exponential: only where a row of the warp does not have all 64 pages)
+    auto for_all_or_some = [&](int left, auto body) {
+      if (__all_sync(0xffffffffu, left >= kPart || row >= rows)) body(std::false_type{}); else body(std::true_type{});
+    };
     const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
     uint32_t done[2] = {0, 0};
     auto wait_for = [&](int tile) {
@@ -205,33 +211,38 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
         uint32_t v[2][32];
         logits(tile, part, v);
         const int left = count - first;
-        // (the maximum of those that are numbers: one that is not makes the sum one)
-        float2 more = make_float2(-INFINITY, 0.f);
-        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        for_all_or_some(left, [&](auto some) {
+          constexpr bool kSome = decltype(some)::value;
+          // (the maximum of those that are numbers: one that is not makes the sum one)
+          float2 more = make_float2(-INFINITY, 0.f);
+          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < kPart; i += 2) {
-          float x, y;
-          unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1])), scale2), x, y);
-          if (i >= left) x = -INFINITY;
-          if (i + 1 >= left) y = -INFINITY;
-          v[i >> 5][i & 31] = __float_as_uint(x);
-          v[i >> 5][(i & 31) + 1] = __float_as_uint(y);
-          tops[i / 2 & 3] = fmax3(tops[i / 2 & 3], x, y);
-        }
-        more.x = fmaxf(fmax3(tops[0], tops[1], tops[2]), tops[3]);
-        const float off = more.x == -INFINITY ? 0.f : more.x;
-        const uint64_t off2 = pack_f32x2(-off, -off);
-        uint64_t sums[2] = {0, 0};
+          for (int i = 0; i < kPart; i += 2) {
+            float x, y;
+            unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1])), scale2), x, y);
+            if (kSome) {
+              if (i >= left) x = -INFINITY;
+              if (i + 1 >= left) y = -INFINITY;
+            }
+            v[i >> 5][i & 31] = __float_as_uint(x);
+            v[i >> 5][(i & 31) + 1] = __float_as_uint(y);
+            tops[i / 2 & 3] = fmax3(tops[i / 2 & 3], x, y);
+          }
+          more.x = fmaxf(fmax3(tops[0], tops[1], tops[2]), tops[3]);
+          const float off = more.x == -INFINITY ? 0.f : more.x;
+          const uint64_t off2 = pack_f32x2(-off, -off);
+          uint64_t sums[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < kPart; i += 2) {
+          for (int i = 0; i < kPart; i += 2) {
+            float x, y;
+            unpack_f32x2(add_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1])), off2), x, y);
+            sums[i / 2 & 1] = add_f32x2(sums[i / 2 & 1], pack_f32x2(ex2_approx(x), ex2_approx(y)));
+          }
           float x, y;
-          unpack_f32x2(add_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][i & 31]), __uint_as_float(v[i >> 5][(i & 31) + 1])), off2), x, y);
-          sums[i / 2 & 1] = add_f32x2(sums[i / 2 & 1], pack_f32x2(ex2_approx(x), ex2_approx(y)));
-        }
-        float x, y;
-        unpack_f32x2(add_f32x2(sums[0], sums[1]), x, y);
-        more.y = x + y;
-        known = join(known, more);
+          unpack_f32x2(add_f32x2(sums[0], sums[1]), x, y);
+          more.y = x + y;
+          known = join(known, more);
+        });
       }
       if (tile < again) give_back(tile);
     }
@@ -268,17 +279,20 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
           float* to = shares + row * stride + wide / 2 * half + (rounds == 1 ? part : 0);
           uint32_t v[2][32];
           logits(tile, part, v);
+          for_all_or_some(left, [&](auto some) {
+            constexpr bool kSome = decltype(some)::value;
 #pragma unroll
-          for (int i = 0; i < kPart; i += 4) {
-            float e[4];
+            for (int i = 0; i < kPart; i += 4) {
+              float e[4];
 #pragma unroll
-            for (int k = 0; k < 4; k += 2) {
-              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][(i & 31) + k]), __uint_as_float(v[i >> 5][(i & 31) + k + 1])), scale2, off2), e[k], e[k + 1]);
-              e[k] = i + k < left ? ex2_approx(e[k]) : 0.f;
-              e[k + 1] = i + k + 1 < left ? ex2_approx(e[k + 1]) : 0.f;
+              for (int k = 0; k < 4; k += 2) {
+                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i >> 5][(i & 31) + k]), __uint_as_float(v[i >> 5][(i & 31) + k + 1])), scale2, off2), e[k], e[k + 1]);
+                e[k] = !kSome || i + k < left ? ex2_approx(e[k]) : 0.f;
+                e[k + 1] = !kSome || i + k + 1 < left ? ex2_approx(e[k + 1]) : 0.f;
+              }
+              *reinterpret_cast<float4*>(to + i) = make_float4(e[0], e[1], e[2], e[3]);
             }
-            *reinterpret_cast<float4*>(to + i) = make_float4(e[0], e[1], e[2], e[3]);
-          }
+          });
         }
         meet<1, kSumThreads>();
         // (of a round of two halves of 64 pages, the second is 128 pages further on)
