@@ -6,13 +6,15 @@
 // 32 x 65536 keys 23 us, 15.5 this way.  A sum of heads, not a maximum, because all heads attend to what is selected.)
 // What bounds it, 32 x 65536 keys of 128 heads, 15.5 us, 26 K clk a block: 2.5 K until the length is there; the first means 4.5 K later; then 37.7 MB of means at
 // 6.4 TB/s until 16.5 K; statistics 2.8 K and shares 2.9 K (2 K each are exponentials, sixteen a clock), exchange 1.4 K, sums 1.9 K.  Short contexts (8 x 1.5-4 K, 16 heads) take 6.5 us, a
-// launch and that chain; long ragged ones (12 x 9-262 K, two tokens, 26.9 us) wait for the longest sequence, of whose tiles half are multiplied twice.
+// launch and that chain; long ragged ones (12 x 9-262 K, two tokens, 25.2 us) wait for the longest sequences, which come first where not all clusters have room (26.9 in order, by clusters
+// of four; 24 x 9-262 K 40.3 -> 34.1; with smaller clusters it is of no use: 120 x 1-65 K 36.2 in order, 39.4 the longest first).
 // One lane a scheduler is all that a loading warp gets, so that every address is at hand before the loop (1200 -> 350 clk for an operand place of a short context).
 // Tried: Q kept in shared memory beside a ring of 64 KB (a third of the bytes under way: 16.4 us, 45.7 for the long ragged ones); 16 summing warps (16.1); shares of the last
 // tile kept from the first pass over its logits (0.5 less, 1.5 more for the long ragged ones).
 //
 // select: a block for a query token.  4.5 us for 512 pages, 10.3 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
 // runs once, which rolled loops of 256 threads do in less time than unrolled ones of 1024 (up to 2048 pages; 16 K pages take 1024 threads 10.3 us).
+#include <climits>
 #include <type_traits>
 
 #include "../../include/amla.h"
@@ -69,11 +71,12 @@ __device__ const uint4 zero_row[kDqk / 8] = {};
 
 }  // namespace
 
-__global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScoreParams p, int blocks) {
+__global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScoreParams p, int blocks, int longest_first) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
   const int tokens_most = tokens_of_item(p.Sq, p.H), items = (p.Sq + tokens_most - 1) / tokens_most;
-  const int rank = blockIdx.x % blocks, item = blockIdx.x / blocks % items, b = blockIdx.x / blocks / items;
+  const int rank = blockIdx.x % blocks, item = blockIdx.x / blocks % items;
+  int b = blockIdx.x / blocks / items;
   const int t0 = item * tokens_most, tokens = min(p.Sq - t0, tokens_most), rows = tokens * p.H;
   const uint32_t base = smem_u32(smem), bars = base + kOffBars, tmem_slot = bars + 256 - 8;
   auto bar = [&](int i) { return bars + 8u * i; };
@@ -93,6 +96,22 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
   const uint32_t tmem = ld_shared_b32(tmem_slot);
   behind_the_kernel_in_front();
   if (blockIdx.x == 0 && tid == 0) *p.status = kStatusOk;
+  if (longest_first) {                                         // the b-th longest sequence, of up to as many as there are threads
+    int4* lens = reinterpret_cast<int4*>(smem);
+    int* found = reinterpret_cast<int*>(smem + kOffLse);
+    const int mine = tid < p.B ? ldg_here(p.seqlens + tid) : INT_MIN;
+    reinterpret_cast<int*>(lens)[tid] = mine;
+    __syncthreads();
+    int before = 0;
+    for (int i = 0; i < (p.B + 3) / 4; ++i) {
+      const int4 l = lens[i];
+      before += (l.x > mine || (l.x == mine && 4 * i < tid)) + (l.y > mine || (l.y == mine && 4 * i + 1 < tid)) + (l.z > mine || (l.z == mine && 4 * i + 2 < tid)) +
+                (l.w > mine || (l.w == mine && 4 * i + 3 < tid));
+    }
+    if (tid < p.B && before == b) *found = tid;
+    __syncthreads();
+    b = *found;
+  }
 
   const int most = candidates(seen_by(p.seqlens, b, p.Sq, t0 + tokens - 1, p.width));
   const int share = ((most + blocks - 1) / blocks + 15) / 16 * 16, page0 = min(rank * share, most), here = min(share, most - page0);
@@ -514,13 +533,14 @@ int clusters_of_16() {
   return k.load(std::memory_order_acquire) - 1;
 }
 
-// Blocks in a cluster: as many as there are SMs for, but none that would have less than 64 pages of the longest sequence, and sixteen only where blocks of eight
-// would have more than a tile and all clusters have room at once.  Measured (blocks 1 / 2 / 4 / 8 / 16, us): 32 x 65536 keys 38.3 / 20.7 / 15.7 / 31.2; 128 x 16384 17.9 / 23.8 /
-// 36.6 / 77.3; 64 x 1-65 K 38.5 / 21.2 / 25.6 / 45.5; 16 x 65536 of two tokens 35.4 / 18.4 / 12.9 / 28.1; 1 x 262144 100 / 52 / 28 / 14.4 / 10.8; 8 x 262144, of
-// whose clusters of sixteen seven have room, - / - / - / 20.6 / 27.8.
+// Blocks in a cluster: as many as there are SMs for, but none that would have less than 64 pages of the longest sequence; more than that where a block would else have more than
+// two tiles (which are multiplied twice), the longest sequences first then; and sixteen only where blocks of eight would have more than a tile and all clusters have room at once.
+// Measured (blocks 1 / 2 / 4 / 8 / 16, us): 32 x 65536 keys 38.3 / 20.7 / 15.7 / 31.2; 128 x 16384 17.9 / 23.8 / 36.6 / 77.3; 64 x 1-65 K 38.5 / 21.2 / 25.6 / 45.5; 16 x 65536 of two
+// tokens 35.4 / 18.4 / 12.9 / 28.1; 1 x 262144 100 / 52 / 28 / 14.4 / 10.8; 8 x 262144, of whose clusters of sixteen seven have room, - / - / - / 20.6 / 27.8; 24 x 262144 - / 79.0 /
+// 46.4 / 44.7; 60 x 131072 - / 50.5 / 48.5 / 61.9; 120 x 65536 - / 49.5 / 61.1 / 85.8.
 int score_blocks(int items, int width, int sms) {
   int blocks = 1;
-  while (blocks < 8 && static_cast<long long>(items) * 2 * blocks <= sms && width > 64 * blocks) blocks *= 2;
+  while (blocks < 8 && width > 64 * blocks && (static_cast<long long>(items) * 2 * blocks <= sms || width > 2 * kTilePages * blocks)) blocks *= 2;
   if (blocks == 8 && width > 8 * kTilePages && items <= sms / 16 && items <= clusters_of_16()) blocks = 16;
   return blocks;
 }
@@ -535,7 +555,8 @@ cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t strea
   const int blocks = score_blocks(items, p.width, sms);
   cudaLaunchAttribute attr[2];
   const cudaLaunchConfig_t cfg = score_config(items, blocks, stream, attr);
-  return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, blocks);
+  const int longest_first = blocks == 8 && items * 8 > sms && p.B <= kThreads;
+  return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, blocks, longest_first);
 }
 
 namespace {

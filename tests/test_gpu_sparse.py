@@ -104,6 +104,14 @@ def test_scores_of_a_long_context():
     check_scores([400000, 130000], 2, 16)
 
 
+@pytest.mark.parametrize("B,Sq,H", [(24, 1, 16), (12, 2, 128), (40, 1, 5), (3, 8, 128)])
+def test_scores_of_more_clusters_than_fit_at_once(B, Sq, H):
+    # (the longest sequences come first then: several of one length, some of none, the longest last)
+    rng = np.random.default_rng(B)
+    lens = [int(n) for n in rng.choice([0, 1, 65, 4000, 4000, 30000, 30000, 64 * 900], B - 1)] + [64 * 2150 + 9]
+    check_scores(lens, Sq, H)
+
+
 def test_scores_twice_are_the_same_bits():
     q, means = torch.randn(4, 2, 128, 576, device="cuda").bfloat16(), torch.randn(4000, 576, device="cuda").bfloat16()
     table, lens = torch.randperm(4000, device="cuda").int().view(4, 1000), torch.tensor([64000, 5, 30000, 63000], dtype=torch.int32, device="cuda")

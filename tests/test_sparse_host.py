@@ -272,7 +272,7 @@ def test_kernels_read_behind_the_wait_and_promise_nothing(name, kernels):
 
 def test_a_scoring_kernel_that_gives_up_waits_for_its_products_and_its_peers():
     text = re.sub(r"//[^\n]*", "", open(os.path.join(build.CSRC, "amla_select.cu")).read())
-    kernel = text[text.index("page_scores_kernel(const ScoreParams p, int blocks)"):text.index("constexpr int kHeldPages")]
+    kernel = text[text.index("page_scores_kernel(const ScoreParams p, int blocks, int longest_first)"):text.index("constexpr int kHeldPages")]
     role = kernel[kernel.index("wid == kMmaWarp) {\n    if (elect_one())"):kernel.index("    const int quarter")]
     assert re.search(r"if \(!ok\) \{\s*mma_commit\(bar\(X_GIVE_UP\)\);\s*mbar_wait\(bar\(X_GIVE_UP\), 0\);", role)
     assert "cp_async_wait_all();" in kernel[:kernel.index("wid == kMmaWarp) {\n    if (elect_one())")]
