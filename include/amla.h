@@ -252,7 +252,8 @@ int amla_pages_compact(void* cache, long long page_bytes, int32_t* block_table, 
  *   format       AMLA_CACHE_BF16 (bf16 [num_blocks, 64, 576]), AMLA_CACHE_E4M3 (uint8 [num_blocks, 64, 576], value = e4m3 * kv_scale) or
  *                AMLA_CACHE_FP4 (as for amla_cache_store_fp4); kv_scale 2^-100 .. 2^100, not used by bf16
  *   kv, starts   the batch's tokens, rows of 576 bf16 `row_stride` elements apart, and which of them are whose: as for amla_cache_store_fp4, and so
- *                are the tokens that are not stored.  Two tokens of a call must not have the same place.
+ *                are the tokens that are not stored (a row that amla_pages_reserve refused is left out by a length of 0).  Two tokens of a call must not have
+ *                the same place.
  *   cos_sin      fp32 [n_positions, 64], 16-byte aligned: for each position the cosines of its 32 angles, then their sines
  *   positions    int32 [n_tokens], or NULL: the position of a token is its place in its sequence.  A token whose position is outside
  *                [0, n_positions) is not stored, and its queries are left as they are.

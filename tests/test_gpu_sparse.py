@@ -95,6 +95,29 @@ def test_scores_of_other_sizes(size, scale):
     check_scores([3000, 700], 1, 64, scale=scale, size=size)
 
 
+def test_means_beyond_32_bits():
+    blocks, W = 3_900_000, 20                            # 4.5 GB of means
+    means = torch.empty((blocks, 576), dtype=torch.bfloat16, device="cuda")
+    few = torch.randn(W, 576, device="cuda").bfloat16()
+    means[-W:] = few
+    means[:W].zero_()
+    q, lens = torch.randn(1, 1, 64, 576, device="cuda").bfloat16(), torch.tensor([64 * W], dtype=torch.int32, device="cuda")
+    table = torch.arange(W, dtype=torch.int32, device="cuda").view(1, W)
+    want = sparse.page_scores(q, few, table, lens, SCALE)
+    assert torch.equal(sparse.page_scores(q, means, table + (blocks - W), lens, SCALE), want) and float(want.sum()) > 63
+
+
+def test_queries_beyond_32_bits():
+    B = 30000                                            # 4.4 GB of queries
+    q = torch.zeros(B, 1, 128, 576, dtype=torch.bfloat16, device="cuda")
+    few, means = torch.randn(1, 1, 128, 576, device="cuda").bfloat16(), torch.randn(4, 576, device="cuda").bfloat16()
+    q[-1] = few[0]
+    table, lens = torch.arange(4, dtype=torch.int32, device="cuda").expand(B, 4).contiguous(), torch.full((B,), 250, dtype=torch.int32, device="cuda")
+    got = sparse.page_scores(q, means, table, lens, SCALE)
+    want = sparse.page_scores(few, means, table[:1], lens[:1], SCALE)
+    assert torch.equal(got[-1], want[0]) and torch.allclose(got[:-1, :, :3], torch.full_like(got[:-1, :, :3], 128 / 3), rtol=1e-6) and not got[..., 3].any()
+
+
 def test_scores_many_sequences():
     rng = np.random.default_rng(5)
     check_scores([int(n) for n in rng.integers(0, 2000, 300)], 1, 24)
