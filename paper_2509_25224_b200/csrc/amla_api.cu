@@ -518,7 +518,7 @@ extern "C" int amla_page_scores(const void* q, const void* means, const int32_t*
   char* ws = static_cast<char*>(workspace);
   const ScoreParams p{static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(means), block_table, seqlens, softmax_scale * kLog2e, B, Sq, H, num_blocks,
                       max_blocks_per_seq, scores, reinterpret_cast<int*>(ws)};
-  return launched(launch_page_scores(p, sms, static_cast<cudaStream_t>(cuda_stream)));
+  return launched(launch_page_scores(p, nullptr, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 extern "C" int amla_pages_select(const float* scores, const int32_t* block_table, const int32_t* seqlens, int B, int Sq, int max_blocks_per_seq, int keep, int sink, int recent,
@@ -577,16 +577,20 @@ extern "C" int amla_mla_decode_sparse(int format, const void* q, const void* kv_
   int32_t* table = reinterpret_cast<int32_t*>(ws + lay.table_off);
   int32_t* lens = reinterpret_cast<int32_t*>(ws + lay.lens_off);
   float* scores = reinterpret_cast<float*>(ws + lay.scores_off);
+  const SelectParams select{all ? nullptr : scores, block_table, seqlens, B, Sq, max_blocks_per_seq, keep, sink, recent, table, lens, nullptr,
+                            all ? reinterpret_cast<int*>(ws + kScoreStatusOff) : nullptr};
+  const bool together = !all && scores_select(max_blocks_per_seq);
   if (!all) {
     const ScoreParams p{static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(means), block_table, seqlens, softmax_scale * kLog2e, B, Sq, H, num_blocks,
                         max_blocks_per_seq, scores, reinterpret_cast<int*>(ws + kScoreStatusOff)};
-    rc = launched(launch_page_scores(p, sms, stream));
+    rc = launched(launch_page_scores(p, together ? &select : nullptr, sms, stream));
     if (rc != AMLA_OK) return rc;
   }
-  rc = launched(launch_pages_select(SelectParams{all ? nullptr : scores, block_table, seqlens, B, Sq, max_blocks_per_seq, keep, sink, recent, table, lens, nullptr,
-                                                all ? reinterpret_cast<int*>(ws + kScoreStatusOff) : nullptr}, stream));
-  if (rc != AMLA_OK) return rc;
-  const int front = all ? 1 : 2;
+  if (!together) {
+    rc = launched(launch_pages_select(select, stream));
+    if (rc != AMLA_OK) return rc;
+  }
+  const int front = all || together ? 1 : 2;
   if (format == AMLA_CACHE_FP4)
     rc = amla_mla_decode_fp4(q, kv_cache, kv_scale, table, lens, softmax_scale, B * Sq, 1, H, num_blocks, keep, out, lse, ws, lay.decode_bytes, cuda_stream);
   else if (format == AMLA_CACHE_E4M3)      // (up to 128 rows: widened on their way in)

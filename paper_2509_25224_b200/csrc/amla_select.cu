@@ -12,8 +12,8 @@
 // Tried: Q kept in shared memory beside a ring of 64 KB (a third of the bytes under way: 16.4 us, 45.7 for the long ragged ones); 16 summing warps (16.1); shares of the last
 // tile kept from the first pass over its logits (0.5 less, 1.5 more for the long ragged ones).
 //
-// select: a block for a query token.  4.5 us for 512 pages, 10.3 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
-// runs once, which rolled loops of 256 threads do in less time than unrolled ones of 1024 (up to 2048 pages; 16 K pages take 1024 threads 10.3 us).
+// select: a block for a query token; in a sparse call one of the scoring's cluster (32 x 8-65 K keys 48.8 -> 48.2 us, and 2 us of host time).  By itself 4.5 us for 512 pages, 10.3 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
+// runs once, which rolled loops of 256 threads do in less time than unrolled ones of 1024 (up to 2048 pages).
 #include <climits>
 #include <type_traits>
 
@@ -37,6 +37,145 @@ __device__ __forceinline__ int seen_by(const int32_t* seqlens, int b, int Sq, in
 // pages in front of the one that holds the token's own position
 __device__ __forceinline__ int candidates(int seen) { return seen > 0 ? (seen - 1) / kPage : 0; }
 
+// Selection, by a block.
+constexpr int kHeldPages = 24576;                              // up to so many pages a row's scores, as their order, and what is chosen of them are kept in shared memory
+
+// A number's place in the order of scores: larger for larger ones, the same for both zeros, that of -infinity for a NaN.
+__device__ __forceinline__ uint32_t order_of(float f) {
+  if (f != f) return 0x007fffffu;
+  const uint32_t u = __float_as_uint(f + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+template <int kSelectThreads>
+struct __align__(16) SelectScratch {
+  int counts[4][256];                                          // a table for each of the four times, the largest eight bits first
+  int4 found;                                                  // the next eight bits, how many are wanted of those that have them, how many there are
+  int2 totals[kSelectThreads / 32];
+  uint2 kinds[kSelectThreads];                                 // of 32 pages each: which are taken anyway, and which agree
+  __device__ __forceinline__ void clear() {
+    for (int i = threadIdx.x; i < 1024; i += kSelectThreads) (&counts[0][0])[i] = 0;
+  }
+};
+
+// The choice for query token `row` = b * Sq + t, which sees `seen` keys.  The scores' order is looked at eight bits at a time, from the top: how many of those that
+// agree with the bits found so far have which next eight; the one that is looked for lies in one of these 256, and if all of those are wanted the bits suffice.
+// kHeld: held_keys [width] has the order of the row's scores (written by these threads), and room for [keep] positions behind it.  sm is clear.
+template <int kSelectThreads, bool kHeld>
+__device__ __forceinline__ void select_row(const SelectParams& p, int row, int seen, uint32_t* held_keys, SelectScratch<kSelectThreads>& sm) {
+  const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, count = (seen + kPage - 1) / kPage;
+  const float* scores = p.scores + static_cast<size_t>(row) * p.width;
+  const int32_t* entries = p.block_table + static_cast<size_t>(row / p.Sq) * p.width;
+  int32_t* table = p.table + static_cast<size_t>(row) * p.keep;
+  int32_t* chosen = p.chosen ? p.chosen + static_cast<size_t>(row) * p.keep : nullptr;
+  const int kept = min(count, p.keep);
+  for (int i = kept + tid; i < p.keep; i += kSelectThreads) {
+    table[i] = -1;
+    if (chosen) chosen[i] = -1;
+  }
+  if (tid == 0) p.lens[row] = seen - (count - kept) * kPage;
+  if (count <= p.keep) {
+    for (int i = tid; i < count; i += kSelectThreads) {
+      table[i] = entries[i];
+      if (chosen) chosen[i] = i;
+    }
+    return;
+  }
+  const int first = p.sink, end = count - p.recent;            // the others; more than are wanted
+  auto key = [&](int i) { return kHeld ? held_keys[i] : order_of(scores[i]); };
+  int left = p.keep - p.sink - p.recent, shift = 32;           // wanted of those that agree in the bits from `shift` on
+  uint32_t prefix = 0;
+  __syncthreads();
+  if (left > 0) {
+    int there;
+    do {
+      shift -= 8;
+      int* const table_of = sm.counts[shift >> 3];
+#pragma unroll 1
+      for (int i = first + tid; i < end; i += kSelectThreads) {
+        const uint32_t k = key(i);
+        if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&table_of[~(k >> shift) & 255], 1);
+      }
+      __syncthreads();
+      if (wid == 0) {                                          // lane 0 has the largest eight
+        const int4 a = *reinterpret_cast<const int4*>(table_of + 8 * lane), c = *reinterpret_cast<const int4*>(table_of + 8 * lane + 4);
+        const int mine[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w}, sum = ((a.x + a.y) + (a.z + a.w)) + ((c.x + c.y) + (c.z + c.w));
+        int above = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, above, o); if (lane >= o) above += x; }
+        above -= sum;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (above < left && left <= above + mine[i]) sm.found = make_int4(255 - 8 * lane - i, left - above, mine[i], 0);
+          above += mine[i];
+        }
+      }
+      __syncthreads();
+      prefix |= static_cast<uint32_t>(sm.found.x) << shift;
+      left = sm.found.y;
+      there = sm.found.z;
+    } while (shift > 0 && left < there);
+  } else {
+    shift = 0;
+    prefix = 0xfffffffeu;                                      // above every score, below the pages that are taken anyway
+  }
+  prefix >>= shift;
+  // Those above, and the first `left` of those that agree.  A warp notes for 32 neighbouring pages which are what, as bits; then a thread has 32 pages.
+  int* const list = kHeld ? reinterpret_cast<int*>(held_keys + p.width) : nullptr;
+  int2 front = make_int2(0, 0);                                // of the pages before these
+  for (int page0 = 0; page0 < count; page0 += 32 * kSelectThreads) {
+    const int pieces = min((count - page0 + 31) / 32, kSelectThreads);
+#pragma unroll 1
+    for (int c = wid; c < pieces; c += kSelectThreads / 32) {
+      const int i = page0 + 32 * c + lane;
+      const uint32_t k = i >= count ? 0u : i < first || i >= end ? 0xffffffffu : key(i) >> shift;      // (what is behind the last page may agree, and is not among the first)
+      const uint32_t take = __ballot_sync(0xffffffffu, k > prefix), same = __ballot_sync(0xffffffffu, k == prefix);
+      if (lane == 0) sm.kinds[c] = make_uint2(take, same);
+    }
+    __syncthreads();
+    const uint2 mine = tid < pieces ? sm.kinds[tid] : make_uint2(0, 0);
+    int2 n = make_int2(__popc(mine.x), __popc(mine.y));
+    const int2 own = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, n.x, o), y = __shfl_up_sync(0xffffffffu, n.y, o);
+      if (lane >= o) { n.x += x; n.y += y; }
+    }
+    if (lane == 31) sm.totals[wid] = n;
+    __syncthreads();
+    const int2 all = lane < kSelectThreads / 32 ? sm.totals[lane] : make_int2(0, 0);
+    int2 others = lane < wid ? all : make_int2(0, 0);          // of the warps in front
+#pragma unroll
+    for (int o = 16; o; o >>= 1) { others.x += __shfl_xor_sync(0xffffffffu, others.x, o); others.y += __shfl_xor_sync(0xffffffffu, others.y, o); }
+    n.x += front.x + others.x - own.x;
+    n.y += front.y + others.y - own.y;
+#pragma unroll 1
+    for (uint32_t bits = mine.x | (n.y < left ? mine.y : 0u); bits; bits &= bits - 1) {
+      const int at = __ffs(bits) - 1, same = n.y + __popc(mine.y & ((1u << at) - 1)), to = n.x + __popc(mine.x & ((1u << at) - 1)) + min(same, left);
+      const int page = page0 + 32 * tid + at;
+      if ((!(mine.x >> at & 1) && same >= left) || to >= p.keep) continue;      // (no more than `keep`, should the scores change meanwhile)
+      if (kHeld) {
+        list[to] = page;
+      } else {
+        table[to] = entries[page];
+        if (chosen) chosen[to] = page;
+      }
+    }
+    if (page0 + 32 * kSelectThreads < count) {
+      front.x += __reduce_add_sync(0xffffffffu, all.x);
+      front.y += __reduce_add_sync(0xffffffffu, all.y);
+    }
+    __syncthreads();
+  }
+  if (kHeld) {
+    for (int i = tid; i < p.keep; i += kSelectThreads) {
+      const int page = min(static_cast<uint32_t>(list[i]), static_cast<uint32_t>(p.width - 1));         // (of a page, whatever a scoring that gave up has left)
+      table[i] = entries[page];
+      if (chosen) chosen[i] = page;
+    }
+  }
+}
+
 // Scores.  An item is some query tokens of a sequence, as many as have 128 rows (a row: a head) between them; a cluster of up to sixteen blocks has an item,
 // a block a share of its pages.  It multiplies the rows by its pages' means, up to 256 pages at a time (a tile), keeps the logits of the
 // last two tiles in tensor memory, sends what it knows of every row (maximum and sum) to the others of the cluster and, with what they know,
@@ -54,6 +193,8 @@ constexpr uint32_t kWorkBytes = 227328, kStatsBytes = kMostBlocks * kTileRows * 
 constexpr uint32_t kOffStats = kWorkBytes - kStatsBytes, kOffKnown = kWorkBytes, kOffLse = kOffKnown + kTileRows * 8;
 constexpr uint32_t kOffHalves = kOffLse + kTileRows * 4, kOffBars = kOffHalves + kTilePages / 2 * 4, kScoreSmem = kOffBars + 256;
 enum { X_FULL = 0, X_EMPTY = kMostStages, X_DONE = 2 * kMostStages, X_FREE = X_DONE + 2, X_STATS = X_FREE + 2, X_GIVE_UP, X_NUM };
+constexpr uint32_t kOffScratch = kWorkBytes - sizeof(SelectScratch<kThreads>);
+static_assert(2 * kHeldPages * 4 <= kOffScratch && kOffScratch % 16 == 0, "selection");
 static_assert(8 * X_NUM + 8 <= 256 && kScoreSmem <= 232448 && kWorkBytes % 1024 == 0, "shared memory");
 static_assert(kTileRows * (kTilePages + 4) * 4 <= kOffStats && kStatsBytes <= kFewBytes && (kWorkBytes - kFewBytes) / (kQBytes + kTilePages * 128) >= 3, "ring");
 
@@ -71,7 +212,7 @@ __device__ const uint4 zero_row[kDqk / 8] = {};
 
 }  // namespace
 
-__global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScoreParams p, int blocks, int longest_first) {
+__global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScoreParams p, int blocks, int longest_first, const SelectParams select) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
   const int tokens_most = tokens_of_item(p.Sq, p.H), items = (p.Sq + tokens_most - 1) / tokens_most;
@@ -350,150 +491,45 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
   tc_fence_before_sync();
   __syncthreads();
   if (wid == kMmaWarp) tmem_dealloc(tmem, 2 * kTilePages);
-  cluster_arrive_relaxed();                                    // (who gave up must not be gone when another's statistics arrive)
-  cluster_wait();
-}
-
-namespace {
-
-constexpr int kHeldPages = 24576;                              // up to so many pages a row's scores, as their order, and what is chosen of them are kept in shared memory
-
-// A number's place in the order of scores: larger for larger ones, the same for both zeros, that of -infinity for a NaN.
-__device__ __forceinline__ uint32_t order_of(float f) {
-  if (f != f) return 0x007fffffu;
-  const uint32_t u = __float_as_uint(f + 0.f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
-}  // namespace
-
-// A block, a query token.  The scores' order is looked at eight bits at a time, from the top: how many of those that agree with the bits found
-// so far have which next eight; the one that is looked for lies in one of these 256, and if all of those are wanted the bits suffice.
-template <int kSelectThreads, bool kHeld>
-__global__ void __launch_bounds__(kSelectThreads) pages_select_kernel(const SelectParams p) {
-  extern __shared__ uint32_t held_keys[];                      // [width], then positions of the chosen pages [keep]
-  __shared__ __align__(16) int counts[4][256];                 // a table for each of the four times, the largest eight bits first
-  __shared__ int4 found;                                       // the next eight bits, how many are wanted of those that have them, how many there are
-  __shared__ int2 totals[kSelectThreads / 32];
-  __shared__ uint2 kinds[kSelectThreads];                      // of 32 pages each: which are taken anyway, and which agree
-  const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31, row = blockIdx.x, b = row / p.Sq, t = row % p.Sq;
-  for (int i = tid; i < 1024; i += kSelectThreads) reinterpret_cast<int*>(counts)[i] = 0;
-  behind_the_kernel_in_front();
-  const float* scores = p.scores + static_cast<size_t>(row) * p.width;
-  const int32_t* entries = p.block_table + static_cast<size_t>(b) * p.width;
-  const int seen = seen_by(p.seqlens, b, p.Sq, t, p.width), count = (seen + kPage - 1) / kPage;
-  if (kHeld && p.width > p.keep) {                             // (all of the row, since the length is on its way)
-#pragma unroll 4
-    for (int i = tid; i < p.width; i += kSelectThreads) held_keys[i] = order_of(scores[i]);
-  }
-  int32_t* table = p.table + static_cast<size_t>(row) * p.keep;
-  int32_t* chosen = p.chosen ? p.chosen + static_cast<size_t>(row) * p.keep : nullptr;
-  const int kept = min(count, p.keep);
-  for (int i = kept + tid; i < p.keep; i += kSelectThreads) {
-    table[i] = -1;
-    if (chosen) chosen[i] = -1;
-  }
-  if (p.clear && row == 0 && tid == 0) *p.clear = kStatusOk;
-  if (tid == 0) p.lens[row] = seen - (count - kept) * kPage;
-  if (count <= p.keep) {
-    for (int i = tid; i < count; i += kSelectThreads) {
-      table[i] = entries[i];
-      if (chosen) chosen[i] = i;
-    }
+  if (select.table == nullptr) {
+    cluster_arrive_relaxed();                                  // (who gave up must not be gone when another's statistics arrive)
+    cluster_wait();
     return;
   }
-  const int first = p.sink, end = count - p.recent;            // the others; more than are wanted
-  auto key = [&](int i) { return kHeld ? held_keys[i] : order_of(scores[i]); };
-  int left = p.keep - p.sink - p.recent, shift = 32;           // wanted of those that agree in the bits from `shift` on
-  uint32_t prefix = 0;
-  __syncthreads();
-  if (left > 0) {
-    int there;
-    do {
-      shift -= 8;
-      int* const table_of = counts[shift >> 3];
+  // The choice, by a block of the cluster for each of the tokens: all of its scores are there, and nobody writes to another's shared memory any more.
+  auto& scratch = *reinterpret_cast<SelectScratch<kThreads>*>(smem + kOffScratch);
+  uint32_t* held_keys = reinterpret_cast<uint32_t*>(smem);
+  scratch.clear();
+  cluster_arrive();
+  cluster_wait();
 #pragma unroll 1
-      for (int i = first + tid; i < end; i += kSelectThreads) {
-        const uint32_t k = key(i);
-        if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&table_of[~(k >> shift) & 255], 1);
-      }
+  for (int k = rank; k < tokens; k += blocks) {
+    const int row = b * p.Sq + t0 + k;
+    for (int i = tid; i < p.width; i += kThreads) held_keys[i] = order_of(p.scores[static_cast<size_t>(row) * p.width + i]);
+    select_row<kThreads, true>(select, row, seen_by(p.seqlens, b, p.Sq, t0 + k, p.width), held_keys, scratch);
+    if (k + blocks < tokens) {
       __syncthreads();
-      if (wid == 0) {                                          // lane 0 has the largest eight
-        const int4 a = *reinterpret_cast<const int4*>(table_of + 8 * lane), c = *reinterpret_cast<const int4*>(table_of + 8 * lane + 4);
-        const int mine[8] = {a.x, a.y, a.z, a.w, c.x, c.y, c.z, c.w}, sum = ((a.x + a.y) + (a.z + a.w)) + ((c.x + c.y) + (c.z + c.w));
-        int above = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, above, o); if (lane >= o) above += x; }
-        above -= sum;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (above < left && left <= above + mine[i]) found = make_int4(255 - 8 * lane - i, left - above, mine[i], 0);
-          above += mine[i];
-        }
-      }
-      __syncthreads();
-      prefix |= static_cast<uint32_t>(found.x) << shift;
-      left = found.y;
-      there = found.z;
-    } while (shift > 0 && left < there);
-  } else {
-    shift = 0;
-    prefix = 0xfffffffeu;                                      // above every score, below the pages that are taken anyway
-  }
-  prefix >>= shift;
-  // Those above, and the first `left` of those that agree.  A warp notes for 32 neighbouring pages which are what, as bits; then a thread has 32 pages.
-  int* const list = kHeld ? reinterpret_cast<int*>(held_keys + p.width) : nullptr;
-  int2 front = make_int2(0, 0);                                // of the pages before these
-  for (int page0 = 0; page0 < count; page0 += 32 * kSelectThreads) {
-    const int pieces = min((count - page0 + 31) / 32, kSelectThreads);
-#pragma unroll 1
-    for (int c = wid; c < pieces; c += kSelectThreads / 32) {
-      const int i = page0 + 32 * c + lane;
-      const uint32_t k = i >= count ? 0u : i < first || i >= end ? 0xffffffffu : key(i) >> shift;      // (what is behind the last page may agree, and is not among the first)
-      const uint32_t take = __ballot_sync(0xffffffffu, k > prefix), same = __ballot_sync(0xffffffffu, k == prefix);
-      if (lane == 0) kinds[c] = make_uint2(take, same);
-    }
-    __syncthreads();
-    const uint2 mine = tid < pieces ? kinds[tid] : make_uint2(0, 0);
-    int2 n = make_int2(__popc(mine.x), __popc(mine.y));
-    const int2 own = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, n.x, o), y = __shfl_up_sync(0xffffffffu, n.y, o);
-      if (lane >= o) { n.x += x; n.y += y; }
-    }
-    if (lane == 31) totals[wid] = n;
-    __syncthreads();
-    const int2 all = lane < kSelectThreads / 32 ? totals[lane] : make_int2(0, 0);
-    int2 others = lane < wid ? all : make_int2(0, 0);          // of the warps in front
-#pragma unroll
-    for (int o = 16; o; o >>= 1) { others.x += __shfl_xor_sync(0xffffffffu, others.x, o); others.y += __shfl_xor_sync(0xffffffffu, others.y, o); }
-    n.x += front.x + others.x - own.x;
-    n.y += front.y + others.y - own.y;
-#pragma unroll 1
-    for (uint32_t bits = mine.x | (n.y < left ? mine.y : 0u); bits; bits &= bits - 1) {
-      const int at = __ffs(bits) - 1, same = n.y + __popc(mine.y & ((1u << at) - 1)), to = n.x + __popc(mine.x & ((1u << at) - 1)) + min(same, left);
-      const int page = page0 + 32 * tid + at;
-      if ((!(mine.x >> at & 1) && same >= left) || to >= p.keep) continue;      // (no more than `keep`, should the scores change meanwhile)
-      if (kHeld) {
-        list[to] = page;
-      } else {
-        table[to] = entries[page];
-        if (chosen) chosen[to] = page;
-      }
-    }
-    if (page0 + 32 * kSelectThreads < count) {
-      front.x += __reduce_add_sync(0xffffffffu, all.x);
-      front.y += __reduce_add_sync(0xffffffffu, all.y);
-    }
-    __syncthreads();
-  }
-  if (kHeld) {
-    for (int i = tid; i < p.keep; i += kSelectThreads) {
-      table[i] = entries[list[i]];
-      if (chosen) chosen[i] = list[i];
+      scratch.clear();
     }
   }
+}
+
+// A block, a query token.
+template <int kSelectThreads, bool kHeld>
+__global__ void __launch_bounds__(kSelectThreads) pages_select_kernel(const SelectParams p) {
+  extern __shared__ uint32_t held_keys[];
+  __shared__ SelectScratch<kSelectThreads> scratch;
+  const int row = blockIdx.x;
+  scratch.clear();
+  behind_the_kernel_in_front();
+  const int seen = seen_by(p.seqlens, row / p.Sq, p.Sq, row % p.Sq, p.width);
+  if (kHeld && p.width > p.keep) {                             // (all of the row, since the length is on its way)
+    const float* scores = p.scores + static_cast<size_t>(row) * p.width;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < p.width; i += kSelectThreads) held_keys[i] = order_of(scores[i]);
+  }
+  if (p.clear && row == 0 && threadIdx.x == 0) *p.clear = kStatusOk;
+  select_row<kSelectThreads, kHeld>(p, row, seen, held_keys, scratch);
 }
 
 namespace {
@@ -547,7 +583,7 @@ int score_blocks(int items, int width, int sms) {
 
 }  // namespace
 
-cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t stream) {
+cudaError_t launch_page_scores(const ScoreParams& p, const SelectParams* select, int sms, cudaStream_t stream) {
   static std::atomic<uint64_t> done{0};
   const int items = p.B * ((p.Sq + tokens_of_item(p.Sq, p.H) - 1) / tokens_of_item(p.Sq, p.H));
   const cudaError_t err = allow_shared(page_scores_kernel, done, kScoreSmem);
@@ -556,7 +592,7 @@ cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t strea
   cudaLaunchAttribute attr[2];
   const cudaLaunchConfig_t cfg = score_config(items, blocks, stream, attr);
   const int longest_first = blocks == 8 && items * 8 > sms && p.B <= kThreads;
-  return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, blocks, longest_first);
+  return cudaLaunchKernelEx(&cfg, page_scores_kernel, p, blocks, longest_first, select ? *select : SelectParams{});
 }
 
 namespace {
@@ -571,6 +607,8 @@ cudaError_t launch_select(const SelectParams& p, cudaStream_t stream) {
 }
 
 }  // namespace
+
+bool scores_select(int width) { return width <= kHeldPages; }
 
 cudaError_t launch_pages_select(const SelectParams& p, cudaStream_t stream) {
   if (p.width > kHeldPages) return launch_in_order(pages_select_kernel<1024, false>, dim3(p.B * p.Sq), 1024, 0, stream, p);

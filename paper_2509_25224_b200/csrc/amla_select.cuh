@@ -27,7 +27,9 @@ struct SelectParams {
   int* clear;                    // a status word that no scoring in front has set, or null
 };
 
-cudaError_t launch_page_scores(const ScoreParams& p, int sms, cudaStream_t stream);
+// The scores, and with `select` the choice by them in the same launch (where scores_select says that it can be).
+bool scores_select(int width);
+cudaError_t launch_page_scores(const ScoreParams& p, const SelectParams* select, int sms, cudaStream_t stream);
 cudaError_t launch_pages_select(const SelectParams& p, cudaStream_t stream);
 
 }  // namespace amla

@@ -272,12 +272,13 @@ def test_kernels_read_behind_the_wait_and_promise_nothing(name, kernels):
 
 def test_a_scoring_kernel_that_gives_up_waits_for_its_products_and_its_peers():
     text = re.sub(r"//[^\n]*", "", open(os.path.join(build.CSRC, "amla_select.cu")).read())
-    kernel = text[text.index("page_scores_kernel(const ScoreParams p, int blocks, int longest_first)"):text.index("constexpr int kHeldPages")]
+    kernel = text[text.index("page_scores_kernel(const ScoreParams p, int blocks, int longest_first, const SelectParams select)"):text.index("pages_select_kernel(const SelectParams p)")]
     role = kernel[kernel.index("wid == kMmaWarp) {\n    if (elect_one())"):kernel.index("    const int quarter")]
     assert re.search(r"if \(!ok\) \{\s*mma_commit\(bar\(X_GIVE_UP\)\);\s*mbar_wait\(bar\(X_GIVE_UP\), 0\);", role)
     assert "cp_async_wait_all();" in kernel[:kernel.index("wid == kMmaWarp) {\n    if (elect_one())")]
-    last = kernel[kernel.rindex("__syncthreads();"):]
-    assert "tmem_dealloc(" in last and last.index("cluster_arrive_relaxed();") < last.index("cluster_wait();")
+    # all blocks of a cluster meet at the end, whether the block goes on to select or not
+    last = kernel[kernel.rindex("tmem_dealloc("):]
+    assert re.search(r"if \(select\.table == nullptr\) \{\s*cluster_arrive_relaxed\(\);\s*cluster_wait\(\);\s*return;\s*\}", last) and re.search(r"cluster_arrive\(\);\s*cluster_wait\(\);", last)
     # between the barrier behind which tensor memory is allocated and the end nobody returns
     assert "return;" not in kernel[kernel.index("tmem_alloc("):kernel.rindex("tmem_dealloc(")].replace("return s;", "")
 
