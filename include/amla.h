@@ -296,7 +296,7 @@ int amla_page_means(int format, const void* kv_cache, float kv_scale, const int3
  *         table in order of position, lens[r] (int32 [B * Sq]) the number of keys in them (all but the last page are full), chosen[r] (int32 [B * Sq, keep], or NULL) their
  *         positions in block_table[b]; -1 beyond.  The three must not overlap the inputs, nor one another.  table and lens are a block table and lengths for any of the decode
  *         calls on B * Sq sequences of one query token each (q [B, Sq, H, 576] as it lies).
- * decode: all of it: scores, selection, attention.  lse is that of the keys attended to.  Where max_blocks_per_seq <= keep no page is left out and means is not
+ * decode: all of it: scores, selection, attention; format and kv_scale as for amla_cache_append.  lse is that of the keys attended to.  Where max_blocks_per_seq <= keep no page is left out and means is not
  *         read (and may be NULL).
  * A length beyond the table counts as its width.  workspace: 256-byte aligned, at least as many bytes as the size function says (calls that overlap in time need distinct ones); 1 <= Sq <= 8, 1 <= H <= 128, B * max_blocks_per_seq <= 2^28, B * Sq <= 2^23.  The status is read with
  * amla_check_status for scores and amla_sparse_check_status for decode.
@@ -344,7 +344,7 @@ int amla_wait_tries_selftest(void* workspace, int tries, int* report, void* cuda
 int amla_validate_paging_host(const int32_t* block_table, const int32_t* seqlens, int B, int num_blocks,
                               int max_blocks_per_seq, int* bad_seq, int* bad_block);
 
-/* Number of kernels the most recent amla_mla_decode[_ex] call on this thread launched. */
+/* Number of kernels the most recent decode call on this thread launched. */
 int amla_last_launch_count(void);
 
 /* Query rows per work item of the most recent decode call on this thread, which tells the kernel that ran: 32 (the kernel

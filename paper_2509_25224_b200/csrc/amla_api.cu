@@ -437,7 +437,7 @@ extern "C" int amla_mla_decode(const void* q, const void* kv_cache, const int32_
 
 namespace {
 
-// Table entries that a scoring takes: its blocks are counted in 31 bits, and there are up to 16 for 64 entries.
+// Table entries that a scoring takes (far more than there are means in any GPU's memory; counts of rows and blocks stay within 31 bits).
 constexpr long long kMostScored = 1 << 28;
 
 // What a scoring needs of a workspace: its status.

@@ -366,6 +366,27 @@ def test_another_stream():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_two_threads_at_once():
+    import threading
+    work = [workload("bf16", [3000, 1500, 9000], 2, 64, seed=1), workload("fp4", [64 * 300, 77, 5000], 1, 128, seed=2)]
+    args = [(dev_bf16(q), cache, kv_scale, means, dev(table), dev(lens), SCALE, 9, 1, 2) for q, cache, _, kv_scale, means, table, lens in work]
+    want = [sparse.mla_decode_sparse(*a) for a in args]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def call(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(200):
+                out, lse = sparse.mla_decode_sparse(*args[i])
+                if not (torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1])):
+                    wrong.append(i)
+
+    threads = [threading.Thread(target=call, args=(i,)) for i in (0, 1)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert wrong == []
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_a_serving_step_together(fmt):
     """A prompt in chunks, then steps of one and two tokens: what is scored and attended to is what was put in, and shared pages serve both their sequences."""
