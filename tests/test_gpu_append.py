@@ -249,6 +249,29 @@ def test_factors_of_every_size(fmt, size):
     check(fmt, [3, 2], [5, 66], weight=None, kv=kv, kv_scale=size / 3)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_weights_off_16_bytes_give_the_same_bits(fmt, dtype):
+    starts, lens, table, blocks = batch([5, 3], [7, 66])
+    kv, cs = torch.randn(8, 576, device="cuda").bfloat16(), dev(angles(70))
+    room = torch.rand(513, device="cuda").to(dtype)
+    a, b = poisoned(fmt, blocks), poisoned(fmt, blocks)
+    paging.cache_append(kv, dev(starts), a, 0.25, dev(table), dev(lens), cs, norm_weight=room[1:])
+    paging.cache_append(kv, dev(starts), b, 0.25, dev(table), dev(lens), cs, norm_weight=room[1:].clone())
+    assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)) and not torch.equal(a.view(torch.uint8), poisoned(fmt, blocks).view(torch.uint8))
+
+
+def test_no_tokens_and_no_heads():
+    starts, lens, table, blocks = batch([0, 0], [7, 66])
+    cache, cs = poisoned("bf16", blocks), dev(angles(70))
+    empty = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    paging.cache_append(empty(0, 576), dev(starts), cache, 1.0, dev(table), dev(lens), cs, q_pe=empty(0, 16, 64), q=empty(0, 16, 576))
+    paging.page_means(cache, 1.0, dev(table), dev(lens), dev(starts), 0, empty(blocks, 576))
+    assert bool((cache.view(torch.int16) == -1).all())
+    paging.cache_append(torch.ones(2, 576, dtype=torch.bfloat16, device="cuda"), dev(np.array([0, 1, 2], np.int32)), cache, 1.0, dev(table), dev(lens), cs, q_pe=empty(2, 0, 64), q=empty(2, 0, 576))
+    assert int((cache.view(torch.int16) != -1).sum()) == 2 * 576
+
+
 def test_as_the_store_without_norm_and_rotation():
     starts, lens, table, blocks = batch([100, 3, 40], [130, 3, 41])
     kv = dev_bf16(S.bf16(np.random.default_rng(4).standard_normal((143, 576))))
