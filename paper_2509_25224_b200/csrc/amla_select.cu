@@ -12,7 +12,8 @@
 // Tried: Q kept in shared memory beside a ring of 64 KB (a third of the bytes under way: 16.4 us, 45.7 for the long ragged ones); 16 summing warps (16.1); shares of the last
 // tile kept from the first pass over its logits (0.5 less, 1.5 more for the long ragged ones).
 //
-// select: a block for a query token; in a sparse call one of the scoring's cluster (32 x 8-65 K keys 48.8 -> 48.2 us, and 2 us of host time).  By itself 4.5 us for 512 pages, 10.3 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
+// select: a block for a query token; in a sparse call one of the scoring's cluster (32 x 8-65 K keys 48.8 -> 48.2 us, and 2 us of host time), where there are no scores if all pages are kept anyway
+// (32 x 0.2-3 K keys of 128 heads, 64 pages kept: 35.7 -> 28.5 us; 2 x 300 of 16 heads 19.4 -> 12.3).  By itself 4.5 us for 512 pages, 10.3 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
 // runs once, which rolled loops of 256 threads do in less time than unrolled ones of 1024 (up to 2048 pages).
 #include <climits>
 #include <type_traits>
@@ -254,7 +255,10 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
     b = *found;
   }
 
-  const int most = candidates(seen_by(p.seqlens, b, p.Sq, t0 + tokens - 1, p.width));
+  // (in a sparse call that leaves none of the sequence's pages out there is nothing to score)
+  const int seen = seen_by(p.seqlens, b, p.Sq, t0 + tokens - 1, p.width);
+  const int most = select.table != nullptr && seen <= select.keep * static_cast<long long>(kPage) ? 0 : candidates(seen);
+  const bool work = most > 0 || select.table == nullptr;
   const int share = ((most + blocks - 1) / blocks + 15) / 16 * 16, page0 = min(rank * share, most), here = min(share, most - page0);
   const int tiles = (here + kTilePages - 1) / kTilePages, again = max(tiles - 2, 0);
   // the k-th tile to be multiplied: all of them, then those that have left tensor memory, backwards
@@ -264,7 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
   cluster_wait();
   bool ok = (base & 1023u) == 0;                               // (the swizzled tiles assume a 1024-byte aligned window)
 
-  if (wid < kLoadWarps) {
+  if (!work) {
+  } else if (wid < kLoadWarps) {
     // a thread brings 16 bytes of every 16th row of either operand (rows that there are not: whatever is there, in rows of the result that nobody reads)
     const int j = tid & 7, r0 = tid >> 3;
     const uint32_t dst = base + sw128_offset(r0, j);           // (16 rows further on the swizzle is the same)
@@ -332,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
     const int quarter = wid & 3, half = (wid - kLoadWarps) >> 2, mine = (wid - kLoadWarps) * 32 + lane, row = 32 * quarter + lane;
     const int token = min(row / p.H, tokens - 1), count = row < rows ? min(candidates(seen_by(p.seqlens, b, p.Sq, t0 + token, p.width)) - page0, here) : 0;
     float* const out = p.scores + (static_cast<size_t>(b) * p.Sq + t0) * p.width;
-    for (int k = 0; k < tokens; ++k)                           // pages that are not scored
+    for (int k = 0; k < tokens && select.table == nullptr; ++k)                    // pages that are not scored (the selection reads none of them)
       for (int i = candidates(seen_by(p.seqlens, b, p.Sq, t0 + k, p.width)) + rank * kSumThreads + mine; i < p.width; i += blocks * kSumThreads) out[static_cast<size_t>(k) * p.width + i] = 0.f;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + kTilePages / 2 * half;
     auto logits = [&](int tile, int part, uint32_t (&v)[2][32]) {
@@ -504,9 +509,9 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
   cluster_wait();
 #pragma unroll 1
   for (int k = rank; k < tokens; k += blocks) {
-    const int row = b * p.Sq + t0 + k;
-    for (int i = tid; i < p.width; i += kThreads) held_keys[i] = order_of(p.scores[static_cast<size_t>(row) * p.width + i]);
-    select_row<kThreads, true>(select, row, seen_by(p.seqlens, b, p.Sq, t0 + k, p.width), held_keys, scratch);
+    const int row = b * p.Sq + t0 + k, sees = seen_by(p.seqlens, b, p.Sq, t0 + k, p.width), scored = work ? candidates(sees) : 0;
+    for (int i = tid; i < scored; i += kThreads) held_keys[i] = order_of(p.scores[static_cast<size_t>(row) * p.width + i]);
+    select_row<kThreads, true>(select, row, sees, held_keys, scratch);
     if (k + blocks < tokens) {
       __syncthreads();
       scratch.clear();

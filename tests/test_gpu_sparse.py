@@ -323,6 +323,12 @@ def test_sparse_decode_of_many_sequences():
     check_sparse("e4m3", [int(n) for n in rng.integers(0, 900, 150)], 1, 128, 4)
 
 
+@pytest.mark.parametrize("Sq,H", [(1, 128), (2, 64), (3, 100), (8, 16)])
+def test_sequences_that_keep_all_beside_some_that_do_not(Sq, H):
+    # (at 5 pages and some, the first tokens keep all and the last do not)
+    check_sparse("bf16", [320, 321, 319 + Sq, 2000, 0, 63, 320 + Sq // 2, 1], Sq, H, 5, 1, 1, width=700)
+
+
 def test_where_no_page_is_left_out_the_means_are_not_read():
     q, cache, values, kv_scale, means, table, lens = workload("bf16", [500, 512, 3], 1, 64)
     args = (dev(table), dev(lens), SCALE)
