@@ -193,10 +193,12 @@ constexpr uint32_t kQBytes = kTileRows * 128;                 // rows of 128 B, 
 constexpr uint32_t kWorkBytes = 227328, kStatsBytes = kMostBlocks * kTileRows * 8, kFewBytes = kTileRows * (kTilePages / 2 + 4) * 4;
 constexpr uint32_t kOffStats = kWorkBytes - kStatsBytes, kOffKnown = kWorkBytes, kOffLse = kOffKnown + kTileRows * 8;
 constexpr uint32_t kOffHalves = kOffLse + kTileRows * 4, kOffBars = kOffHalves + kTilePages / 2 * 4, kScoreSmem = kOffBars + 256;
+// Behind the barriers: which sequence a block has, where the longest come first (a word of its own: a warp may read it late, when others are far ahead), and the address of tensor memory.
+constexpr uint32_t kOffFound = kOffBars + 256 - 16;
 enum { X_FULL = 0, X_EMPTY = kMostStages, X_DONE = 2 * kMostStages, X_FREE = X_DONE + 2, X_STATS = X_FREE + 2, X_GIVE_UP, X_NUM };
 constexpr uint32_t kOffScratch = kWorkBytes - sizeof(SelectScratch<kThreads>);
 static_assert(2 * kHeldPages * 4 <= kOffScratch && kOffScratch % 16 == 0, "selection");
-static_assert(8 * X_NUM + 8 <= 256 && kScoreSmem <= 232448 && kWorkBytes % 1024 == 0, "shared memory");
+static_assert(8 * X_NUM + 16 <= 256 && kScoreSmem <= 232448 && kWorkBytes % 1024 == 0, "shared memory");
 static_assert(kTileRows * (kTilePages + 4) * 4 <= kOffStats && kStatsBytes <= kFewBytes && (kWorkBytes - kFewBytes) / (kQBytes + kTilePages * 128) >= 3, "ring");
 
 __host__ __device__ __forceinline__ int tokens_of_item(int Sq, int H) { return Sq < kTileRows / H ? Sq : kTileRows / H; }
@@ -240,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
   if (blockIdx.x == 0 && tid == 0) *p.status = kStatusOk;
   if (longest_first) {                                         // the b-th longest sequence, of up to as many as there are threads
     int4* lens = reinterpret_cast<int4*>(smem);
-    int* found = reinterpret_cast<int*>(smem + kOffLse);
+    int* found = reinterpret_cast<int*>(smem + kOffFound);
     const int mine = tid < p.B ? ldg_here(p.seqlens + tid) : INT_MIN;
     reinterpret_cast<int*>(lens)[tid] = mine;
     __syncthreads();
