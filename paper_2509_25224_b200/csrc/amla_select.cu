@@ -328,10 +328,14 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
         }
         if (ok) mma_commit(bar(X_DONE + buf));
       }
-      if (!ok) {                                               // what has been issued ends before tensor memory is given back
+      // What has been issued ends before tensor memory is given back, also where those who add it up have given up on it.
+      if (!ok) {
         mma_commit(bar(X_GIVE_UP));
         mbar_wait(bar(X_GIVE_UP), 0);
       }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (ok && used[i] > 0) ok = mbar_wait(bar(X_DONE + i), (used[i] - 1) & 1);
     }
     __syncwarp();
   } else {
