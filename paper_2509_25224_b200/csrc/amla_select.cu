@@ -154,7 +154,7 @@ __device__ __forceinline__ void select_row(const SelectParams& p, int row, int s
     for (uint32_t bits = mine.x | (n.y < left ? mine.y : 0u); bits; bits &= bits - 1) {
       const int at = __ffs(bits) - 1, same = n.y + __popc(mine.y & ((1u << at) - 1)), to = n.x + __popc(mine.x & ((1u << at) - 1)) + min(same, left);
       const int page = page0 + 32 * tid + at;
-      if ((!(mine.x >> at & 1) && same >= left) || to >= p.keep) continue;      // (no more than `keep`, should the scores change meanwhile)
+      if ((!(mine.x >> at & 1) && same >= left) || static_cast<uint32_t>(to) >= static_cast<uint32_t>(p.keep)) continue;      // (no more than `keep`, should the scores change meanwhile)
       if (kHeld) {
         list[to] = page;
       } else {
@@ -193,8 +193,9 @@ constexpr uint32_t kQBytes = kTileRows * 128;                 // rows of 128 B, 
 constexpr uint32_t kWorkBytes = 227328, kStatsBytes = kMostBlocks * kTileRows * 8, kFewBytes = kTileRows * (kTilePages / 2 + 4) * 4;
 constexpr uint32_t kOffStats = kWorkBytes - kStatsBytes, kOffKnown = kWorkBytes, kOffLse = kOffKnown + kTileRows * 8;
 constexpr uint32_t kOffHalves = kOffLse + kTileRows * 4, kOffBars = kOffHalves + kTilePages / 2 * 4, kScoreSmem = kOffBars + 256;
-// Behind the barriers: which sequence a block has, where the longest come first (a word of its own: a warp may read it late, when others are far ahead), and the address of tensor memory.
-constexpr uint32_t kOffFound = kOffBars + 256 - 16;
+// Behind the barriers: which sequence a block has, where the longest come first (a word of its own: a warp may read it late, when others are far ahead), whether a peer's statistics were
+// late, and the address of tensor memory.
+constexpr uint32_t kOffFound = kOffBars + 256 - 16, kOffLate = kOffFound + 4;
 enum { X_FULL = 0, X_EMPTY = kMostStages, X_DONE = 2 * kMostStages, X_FREE = X_DONE + 2, X_STATS = X_FREE + 2, X_GIVE_UP, X_NUM };
 constexpr uint32_t kOffScratch = kWorkBytes - sizeof(SelectScratch<kThreads>);
 static_assert(2 * kHeldPages * 4 <= kOffScratch && kOffScratch % 16 == 0, "selection");
@@ -224,7 +225,9 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
   const int t0 = item * tokens_most, tokens = min(p.Sq - t0, tokens_most), rows = tokens * p.H;
   const uint32_t base = smem_u32(smem), bars = base + kOffBars, tmem_slot = bars + 256 - 8;
   auto bar = [&](int i) { return bars + 8u * i; };
+  int* const late = reinterpret_cast<int*>(smem + kOffLate);   // (the same for all threads behind the barrier at the end)
   if (tid == 0) {
+    *late = 0;
     for (int i = 0; i < kMostStages; ++i) { mbar_init(bar(X_FULL + i), kLoadThreads); mbar_init(bar(X_EMPTY + i), 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(bar(X_DONE + i), 1); mbar_init(bar(X_FREE + i), kSumWarps); }
     mbar_init(bar(X_STATS), 1);
@@ -426,7 +429,9 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
       known = join(known, both[row]);
       const uint32_t at = base + kOffStats + (rank * kTileRows + row) * 8;
       for (int i = 0; i < blocks; ++i) st_async_v2(map_to_cta(at, i), __float_as_uint(known.x), __float_as_uint(known.y), map_to_cta(bar(X_STATS), i));
-      ok = __all_sync(0xffffffffu, mbar_wait<true>(bar(X_STATS), 0) && ok);
+      const bool told = mbar_wait<true>(bar(X_STATS), 0);
+      ok = __all_sync(0xffffffffu, told && ok);
+      if (!told) *late = 1;
       float2 all = stats[row];
       for (int i = 1; i < blocks; ++i) all = join(all, stats[i * kTileRows + row]);
       lse[row] = all.x + log2f(all.y);
@@ -502,17 +507,24 @@ __global__ void __launch_bounds__(kThreads, 1) page_scores_kernel(const ScorePar
   tc_fence_before_sync();
   __syncthreads();
   if (wid == kMmaWarp) tmem_dealloc(tmem, 2 * kTilePages);
-  if (select.table == nullptr) {
+  // The choice, by a block of the cluster for each of the tokens: behind the cluster's barrier all of its scores are there, and nobody writes to another's shared memory any more.
+  auto& scratch = *reinterpret_cast<SelectScratch<kThreads>*>(smem + kOffScratch);
+  uint32_t* held_keys = reinterpret_cast<uint32_t*>(smem);
+  if (*late) {                                                 // (this block has given up on what a peer sends before it comes to the barrier: it must not be gone, nor use the place, before that is in)
+    cluster_arrive();
+    cluster_wait();
+    mbar_wait<true>(bar(X_STATS), 0);
+    if (select.table == nullptr) return;
+    scratch.clear();
+  } else if (select.table == nullptr) {
     cluster_arrive_relaxed();                                  // (who gave up must not be gone when another's statistics arrive)
     cluster_wait();
     return;
+  } else {
+    scratch.clear();
+    cluster_arrive();
+    cluster_wait();
   }
-  // The choice, by a block of the cluster for each of the tokens: all of its scores are there, and nobody writes to another's shared memory any more.
-  auto& scratch = *reinterpret_cast<SelectScratch<kThreads>*>(smem + kOffScratch);
-  uint32_t* held_keys = reinterpret_cast<uint32_t*>(smem);
-  scratch.clear();
-  cluster_arrive();
-  cluster_wait();
 #pragma unroll 1
   for (int k = rank; k < tokens; k += blocks) {
     const int row = b * p.Sq + t0 + k, sees = seen_by(p.seqlens, b, p.Sq, t0 + k, p.width), scored = work ? candidates(sees) : 0;

@@ -35,11 +35,12 @@ def regions(text):
     k = constants(text)
     kernel = text[text.index("page_scores_kernel(const ScoreParams p"):text.index("pages_select_kernel(const SelectParams p)")]
     found = re.search(r"found = reinterpret_cast<int\*>\(smem \+ ([\w\s+-]*)\)", kernel)[1]
+    late = re.search(r"late = reinterpret_cast<int\*>\(smem \+ ([\w\s+-]*)\)", kernel)
     slot = re.search(r"tmem_slot = bars \+ ([\w\s+-]*);", kernel)[1]
     rows, at = k["kTileRows"], k["kOffBars"]
     return {"sequence": (eval(found, {}, k), eval(found, {}, k) + 4), "lengths": (0, 4 * k["kThreads"]), "ring and shares": (0, k["kWorkBytes"]), "known": (k["kOffKnown"], k["kOffKnown"] + 8 * rows),
             "lse": (k["kOffLse"], k["kOffLse"] + 4 * rows), "halves": (k["kOffHalves"], k["kOffHalves"] + 4 * (k["kTilePages"] // 2)), "barriers": (at, at + 8 * k["X_NUM"]),
-            "tensor memory": (at + eval(slot, {}, k), at + eval(slot, {}, k) + 4)}
+            "tensor memory": (at + eval(slot, {}, k), at + eval(slot, {}, k) + 4)} | ({"late": (eval(late[1], {}, k), eval(late[1], {}, k) + 4)} if late else {})
 
 
 def overlapping(found, name):
@@ -71,5 +72,5 @@ def test_a_word_that_is_somebody_elses_would_be_seen(place):
 
 def test_all_that_lives_beside_the_ring_is_apart():
     found = regions(SOURCE)
-    for name in ("known", "lse", "halves", "barriers", "tensor memory"):
+    for name in ("known", "lse", "halves", "barriers", "tensor memory", "late"):
         assert overlapping(found, name) == [], name
