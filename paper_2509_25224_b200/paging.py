@@ -21,12 +21,18 @@ _torch = _int = None
 _sizes: dict = {}                    # workspace bytes by (num_blocks, B)
 
 
-def _ready():
-    """The loaded library (and torch, for the checks)."""
+def _types():
+    """torch, for the checks."""
     global _torch, _int
     if _int is None:
         import torch
         _torch, _int = torch, torch.int32
+
+
+def _ready():
+    """The loaded library (and torch)."""
+    if _int is None:
+        _types()
     return binding._lib if binding._lib is not None else binding.lib()
 
 
@@ -154,6 +160,8 @@ def cache_load_fp4(kv_cache_fp4, kv_scale: float, block_table, seqlens, starts, 
 
 def cache_format(cache) -> int:
     """What a cache's pages hold (AMLA_CACHE_*), told from its shape and type: bf16 [num_blocks, 64, 576], uint8 of that shape (E4M3), uint8 [num_blocks, 20736] (4 bits)."""
+    if _torch is None:
+        _types()
     shape = cache.shape
     if len(shape) == 3 and shape[1] == 64 and shape[2] == 576:
         if cache.dtype is _torch.bfloat16:
