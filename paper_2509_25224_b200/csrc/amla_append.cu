@@ -195,9 +195,13 @@ __device__ __forceinline__ void store_key(const AppendParams& p, const Key& key,
     float r;
     if (m >= 0x1p-126f && m <= 0x1.fffffep127f) {
       r = rsqrtf(m);
-    } else {                                         // squares may leave FP32's range where their root does not
-      const bool small = mean < 1.;
-      r = rsqrtf(static_cast<float>(mean * (small ? 0x1p160 : 0x1p-160))) * (small ? 0x1p80f : 0x1p-80f);
+    } else {                                         // squares may leave FP32's range where their root does not; below 2^-128 so does the root's inverse,
+      const bool small = mean < 1.;                  // and the numbers themselves (which are below 2^-58) take its power of two
+      r = rsqrtf(static_cast<float>(mean * (small ? 0x1p160 : 0x1p-160)));
+      if (!small) r *= 0x1p-80f;
+      else
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i >> 3][i & 7] *= 0x1p80f;
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i >> 3][i & 7] = __fmul_rn(__fmul_rn(x[i >> 3][i & 7], r), w[i >> 3][i & 7]);
