@@ -340,8 +340,8 @@ __global__ void __launch_bounds__(kMeanThreads) page_means_kernel(const void* ca
   if (tid == 0) count = 0;
   __syncthreads();
   for (int i = wid; i < window; i += kMeanThreads / 32) {
-    const int token = blockIdx.x * window + i;
-    if (token >= tokens.n) break;
+    const uint32_t token = blockIdx.x * window + i;
+    if (token >= static_cast<uint32_t>(tokens.n)) break;
     const Place at = place_of_token(tokens, token, lane);
     if (lane == 0 && at.page >= 0 && at.row == kPage - 1) pages[atomicAdd(&count, 1)] = static_cast<int>(at.page);
   }
@@ -461,7 +461,7 @@ extern "C" int amla_page_means(int format, const void* kv_cache, float kv_scale,
   // A block's pages come one after the other: a token a block where there are few, at most 64 (a page of one sequence) where there are many.
   const int window = n_tokens / (148 * 8) < 1 ? 1 : n_tokens / (148 * 8) > kMostWindow ? kMostWindow : n_tokens / (148 * 8);
   const Tokens tokens{starts, block_table, seqlens, B, num_blocks, max_blocks_per_seq, n_tokens};
-  const int grid = (n_tokens + window - 1) / window;
+  const int grid = (n_tokens - 1) / window + 1;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(means);
   const cudaError_t err = format == AMLA_CACHE_BF16   ? launch_in_order(page_means_kernel<AMLA_CACHE_BF16>, dim3(grid), kMeanThreads, 0, stream, kv_cache, kv_scale, tokens, window, out)
