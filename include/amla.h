@@ -288,8 +288,9 @@ int amla_page_means(int format, const void* kv_cache, float kv_scale, const int3
  *
  * scores: scores[b,t,p] = sum_h softmax_p(softmax_scale * q[b,t,h,:] . means[page p of sequence b]) over the pages p in front of the one that holds
  *         the query token's own position, which are full; 0 elsewhere.  It is the heads' attention that a page would have, were all of its keys
- *         their mean.  scores: fp32 [B, Sq, max_blocks_per_seq].  A table entry outside [0, num_blocks) counts as a mean of zeros.  A row of q that
- *         holds a NaN or an infinity, or a page in front whose mean does (one that has never been written, say), makes its token's scores NaN.
+ *         their mean.  scores: fp32 [B, Sq, max_blocks_per_seq].  A table entry outside [0, num_blocks) counts as a mean of zeros.  A NaN
+ *         in a row of q, or in the mean of a page in front (one that has never been written, say), makes its token's scores NaN; infinities go by the
+ *         softmax: a head with a logit of +infinity, or with nothing but -infinity, makes them NaN, and else a logit of -infinity is a share of 0.
  * select: of the pages that a token sees, the first `sink`, the last `recent` (at least 1) and, of the others, those with the largest scores,
  *         `keep` in all (sink + recent <= keep); where scores are equal the lower position comes first, and a NaN counts as -infinity.
  *         Scores of other pages do not matter.  For row r = b * Sq + t: table[r] (int32 [B * Sq, keep]) has the pages' entries of the block

@@ -44,3 +44,45 @@ def test_sparse_decode_of_short_sequences_in_a_wide_table(B, Sq, H):
     # besides.  (Largest here: 4.8 and 6.3.  Where the two add up they pass the 2e-2 that outputs below 2 are held to elsewhere: -4.417 lies 0.0047 from the middle between two bf16 numbers 2^-5 apart.)
     v = abs(values[..., :512]).max()
     compare(out.double().cpu().numpy().reshape(ro.shape), lse.double().cpu().numpy().reshape(rl.shape), ro, rl, tol_abs=2.0 ** -8 * (abs(ro).max() + v))
+
+
+def softmax(x):
+    """By its definition, of numbers and infinities: a logit of -infinity has no share, one of +infinity or nothing but -infinity leaves no numbers."""
+    with np.errstate(invalid="ignore"):
+        e = np.exp(x - x.max())
+        return e / e.sum()
+
+
+@pytest.mark.parametrize("H", [1, 2, 16, 128])
+@pytest.mark.parametrize("signs", [(1, 1), (1, -1), (-1, 1), (-1, -1)])
+@pytest.mark.parametrize("pages", [2, 70, 700])
+def test_infinite_means_follow_the_softmax(H, signs, pages):
+    """(the sign of the queries in the column that is infinite, that of the infinity): what is +infinity makes its head's shares NaN, what is -infinity is no share."""
+    rng = np.random.default_rng(pages)
+    q, m = rng.standard_normal((1, 1, H, 576)), 0.5 * rng.standard_normal((pages + 1, 576))
+    q[..., 7] = abs(q[..., 7]) * signs[0] + signs[0]
+    q, m = S.values(S.bf16(q)), S.values(S.bf16(m))
+    m[pages // 2, 7] = signs[1] * np.inf
+    bits = lambda x: (np.ascontiguousarray(x, np.float32).view(np.uint32) >> 16).astype(np.uint16)  # noqa: E731  (of numbers that bf16 has)
+    table, lens = np.arange(pages + 1, dtype=np.int32)[None], np.array([64 * pages + 1], np.int32)
+    got = sparse.page_scores(dev_bf16(bits(q)), dev_bf16(bits(m)), dev(table), dev(lens), SCALE).double().cpu().numpy()[0, 0]
+    want = sum(softmax(q[0, 0, h] @ m[:pages].T * SCALE) for h in range(H))
+    assert (np.isnan(got[:pages]) == np.isnan(want)).all() and got[pages] == 0
+    if signs[0] != signs[1]:
+        clean = np.delete(m, pages // 2, 0)
+        _, bound = S.scores(q, clean, table[:, :pages], lens - 64, SCALE)
+        assert got[pages // 2] == 0 and (abs(got[:pages] - want) <= bound[0, 0] * want).all()
+    else:
+        assert np.isnan(got[:pages]).all()
+
+
+def test_queries_and_pages_that_are_infinite_throughout():
+    """A head's logits that are -infinity for every page leave no numbers, for its token alone; a sequence's pages that all are so, too."""
+    q, means = torch.ones(1, 2, 4, 576, device="cuda").bfloat16(), torch.ones(6, 576, device="cuda").bfloat16()
+    table, lens = torch.arange(6, device="cuda").int().view(1, 6), torch.tensor([64 * 5 + 2], dtype=torch.int32, device="cuda")
+    q[0, 0, 2] = -float("inf")
+    got = sparse.page_scores(q, means, table, lens, SCALE)[0]
+    assert torch.isnan(got[0, :5]).all() and not torch.isnan(got[1]).any() and not got[:, 5].any()
+    q.fill_(1)
+    means.fill_(-float("inf"))
+    assert torch.isnan(sparse.page_scores(q, means, table, lens, SCALE)[0, :, :5]).all()
