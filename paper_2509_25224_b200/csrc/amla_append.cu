@@ -5,16 +5,16 @@
 // the angles of its position, (x, y) -> (x cos - y sin, y cos + x sin) for 32 pairs; the result is rounded once, to what the cache holds:
 // bf16, E4M3 times one factor, or E2M1 numbers against an E4M3 scale for 16 columns (amla_fp4.cuh).  The queries' 64 columns are rotated
 // by the same angles into their places behind the 512 that the absorbed projection writes.
-// The squares' sum is one of exact numbers in FP64 (a bf16 squared has 16 bits), so that it does not depend on the order, the factor and the
-// products are FP32; products and sums of the rotation are rounded one by one.
+// The squares (exact: a bf16 squared has 16 bits) are added up in FP64, in a fixed order, the factor and the products are FP32; products and sums of the
+// rotation are rounded one by one.
 //
 // A launch and a chain of reads (which sequence, its page, the angles) are what a step's tokens cost: 96 tokens of 128 heads 3.2 us, in which 3.4 MB move; with one
 // block for a token, which looked for its place first, 5.7.  4 x 2048 tokens of 16 heads take 14.4 us (47 MB, 3.3 TB/s; without queries 5.9): queries are pieces of 128 bytes that lie 384
-// and 1152 bytes apart, and 56 to 70 registers a thread leave room for a good half of the 8192 warps at a time.  Heads a warp, 4 / 8 / 16 / 32: 17.3 / 14.4 / 14.3 / 15.9, and for 1024
+// and 1152 bytes apart, and 56 to 68 registers a thread leave room for a good half of the 8192 warps at a time.  Heads a warp, 4 / 8 / 16 / 32: 17.3 / 14.4 / 14.3 / 15.9, and for 1024
 // tokens of 128 heads 13.6 / 11.0 / 9.6 / 11.4.
 //
 // means: the mean of a page's 64 keys, as attention sees them, summed in FP32 in a fixed order and rounded to bf16, which is what the
-// products with the queries take.  3.8 us for a step (one page in 64 is filled), 5.5 for 148 pages: the tokens' places, then a page's bytes.
+// products with the queries take.  3.6 us for a step (one page in 64 is filled), 5.5 for 148 pages: the tokens' places, then a page's bytes.
 #include <cuda_bf16.h>
 
 #include "../../include/amla.h"
@@ -458,7 +458,9 @@ extern "C" int amla_page_means(int format, const void* kv_cache, float kv_scale,
   if (rc != AMLA_OK) return rc;
   if (!means || !aligned(means, 16)) return AMLA_ERR_INVALID_ARG;
   if (n_tokens == 0) return AMLA_OK;
-  // A block's pages come one after the other: a token a block where there are few, at most 64 (a page of one sequence) where there are many.
+  // A block's pages come one after the other: a token a block where there are few, at most 64 (a page of one sequence) where there are many, eight blocks for each of a B200's 148 SMs
+  // in between.  (Tokens a block, 1 / 8 / 32 / 64, us: 96 tokens 3.8 / 3.8 / 5.3 / 9.1; 2048 of one sequence 4.9 / 4.1 / 4.5 / 5.3; 5 x 1900 12.4 / 5.4 / 4.7 / 5.2; 20 x 2048 48.7 / 15.8 / 14.0 / 15.3;
+  // 80 x 2048 176 / 45 / 39 / 37; 1600 x 5 13.4 / 7.4 / 10.0 / 14.0.)
   const int window = n_tokens / (148 * 8) < 1 ? 1 : n_tokens / (148 * 8) > kMostWindow ? kMostWindow : n_tokens / (148 * 8);
   const Tokens tokens{starts, block_table, seqlens, B, num_blocks, max_blocks_per_seq, n_tokens};
   const int grid = (n_tokens - 1) / window + 1;

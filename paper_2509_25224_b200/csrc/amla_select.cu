@@ -4,16 +4,16 @@
 // token's own.  A head's lse needs all of its pages before any share of it is known: blocks of a cluster keep their logits in tensor memory until they have
 // exchanged a maximum and a sum for each row, so that every mean is read once and no logit is written.  (Logits by way of memory, two launches:
 // 32 x 65536 keys 23 us, 15.5 this way.  A sum of heads, not a maximum, because all heads attend to what is selected.)
-// What bounds it, 32 x 65536 keys of 128 heads, 15.5 us, 26 K clk a block: 2.5 K until the length is there; the first means 4.5 K later; then 37.7 MB of means at
-// 6.4 TB/s until 16.5 K; statistics 2.8 K and shares 2.9 K (2 K each are exponentials, sixteen a clock), exchange 1.4 K, sums 1.9 K.  Short contexts (8 x 1.5-4 K, 16 heads) take 6.5 us, a
-// launch and that chain; long ragged ones (12 x 9-262 K, two tokens, 25.2 us) wait for the longest sequences, which come first where not all clusters have room (26.9 in order, by clusters
+// What bounds it, 32 x 65536 keys of 128 heads, 15.4 us, 26 K clk a block: 2.5 K until the length is there; the first means 4.5 K later; then 37.7 MB of means at
+// 6.4 TB/s until 16.5 K; statistics 2.8 K and shares 2.9 K (2 K each are exponentials, sixteen a clock), exchange 1.4 K, sums 1.9 K.  Short contexts (8 x 1.5-4 K, 16 heads) take 6.9 us, a
+// launch and that chain; long ragged ones (12 x 9-262 K, two tokens, 25.4 us) wait for the longest sequences, which come first where not all clusters have room (26.9 in order, by clusters
 // of four; 24 x 9-262 K 40.3 -> 34.1; with smaller clusters it is of no use: 120 x 1-65 K 36.2 in order, 39.4 the longest first).
 // One lane a scheduler is all that a loading warp gets, so that every address is at hand before the loop (1200 -> 350 clk for an operand place of a short context).
 // Tried: Q kept in shared memory beside a ring of 64 KB (a third of the bytes under way: 16.4 us, 45.7 for the long ragged ones); 16 summing warps (16.1); shares of the last
 // tile kept from the first pass over its logits (0.5 less, 1.5 more for the long ragged ones).
 //
 // select: a block for a query token; in a sparse call one of the scoring's cluster (32 x 8-65 K keys 48.8 -> 48.2 us, and 2 us of host time), where there are no scores if all pages are kept anyway
-// (32 x 0.2-3 K keys of 128 heads, 64 pages kept: 35.7 -> 28.5 us; 2 x 300 of 16 heads 19.4 -> 12.3).  By itself 4.5 us for 512 pages, 10.3 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
+// (32 x 0.2-3 K keys of 128 heads, 64 pages kept: 35.7 -> 28.5 us; 2 x 300 of 16 heads 19.4 -> 12.3).  By itself 4.5 us for 512 pages, 10.8 for 16 K: a launch, the length, the scores, and two or three times eight bits of their order; code that
 // runs once, which rolled loops of 256 threads do in less time than unrolled ones of 1024 (up to 2048 pages).
 #include <climits>
 #include <type_traits>
@@ -592,8 +592,10 @@ int clusters_of_16() {
   return k.load(std::memory_order_acquire) - 1;
 }
 
-// Blocks in a cluster: as many as there are SMs for, but none that would have less than 64 pages of the longest sequence; more than that where a block would else have more than
+// Blocks in a cluster: as many as there are SMs for, as long as a block has more than 32 pages of the table's width; more than that where a block would else have more than
 // two tiles (which are multiplied twice), the longest sequences first then; and sixteen only where blocks of eight would have more than a tile and all clusters have room at once.
+// By the table's width, since lengths are not known on the host: in one far wider than its sequences each of them gets a cluster for sequences as long as the table (at 1024 and from 2049 pages, us:
+// 128 x 16384 keys 23.7 and 107, against 17.4 in a table of 256; 64 x 1-65 K 21 and 54; 32 x 65536 15.4 and 33.5; 8 x 1.5-4 K of 16 heads 7.0 and 7.0).
 // Measured (blocks 1 / 2 / 4 / 8 / 16, us): 32 x 65536 keys 38.3 / 20.7 / 15.7 / 31.2; 128 x 16384 17.9 / 23.8 / 36.6 / 77.3; 64 x 1-65 K 38.5 / 21.2 / 25.6 / 45.5; 16 x 65536 of two
 // tokens 35.4 / 18.4 / 12.9 / 28.1; 1 x 262144 100 / 52 / 28 / 14.4 / 10.8; 8 x 262144, of whose clusters of sixteen seven have room, - / - / - / 20.6 / 27.8; 24 x 262144 - / 79.0 /
 // 46.4 / 44.7; 60 x 131072 - / 50.5 / 48.5 / 61.9; 120 x 65536 - / 49.5 / 61.1 / 85.8.
